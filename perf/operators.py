@@ -8,8 +8,8 @@ A case is a dict of plain values with an "op":
             down products, weighted sum (layer.experts_w4)
 
 Packed weights of K outputs and C inputs, both rounded up (K to 16, C to 128), in groups of G
-inputs: `codes`, uint8 [K/16][C/128][4][16][16], holds the 32 codes of row 16 a + r and of inputs
-128 b + 32 i + 8 t + e (i = 0..3, e = 0..7) in the 16 bytes at [a][b][t][r]: 32-bit word i, with
+inputs: `codes`, uint8 [K/16][C/128][16][4][16], holds the 32 codes of row 16 a + r and of inputs
+128 b + 32 i + 8 t + e (i = 0..3, e = 0..7) in the 16 bytes at [a][b][r][t]: 32-bit word i, with
 the code of e in nibble e / 2 (e even) or 4 + e / 2 (e odd).  `scales` and `zeros` are
 [K/16][groups][16] (rows beyond K: scale 0, zero 8).  A code q stands for (q - zero) * scale; without zeros, zero is 8.
 """
@@ -123,7 +123,7 @@ def _packed(gen, case, K, C, batch=()):
     the largest of a group is at the end of the range or next to it."""
     group = case["group"]
     rt, nc, ng = _round_up(K, 16) // 16, _round_up(C, 128) // 128, _groups(C, group)
-    shape = (*batch, rt, nc, 4, 16, 16)
+    shape = (*batch, rt, nc, 16, 4, 16)
     zeros = None
     if case["zeros"]:
         zeros = torch.randint(5, 11, (*batch, rt, ng, 16), generator=gen, device="cuda", dtype=torch.uint8)
@@ -171,9 +171,9 @@ def _unpack(w):
     codes, scales, zeros, K, C, group = w
     *batch, rt, nc, _, _, _ = codes.shape
     nibbles = torch.stack((codes & 15, codes >> 4), -1)                     # of byte 4 i + j: 2 j and 2 j + 1
-    q = nibbles.view(*batch, rt, nc, 4, 16, 4, 2, 4)                        # a b t r i h n: e = 2 n + h
+    q = nibbles.view(*batch, rt, nc, 16, 4, 4, 2, 4)                        # a b r t i h n: e = 2 n + h
     n = len(batch)
-    q = q.permute(*range(n), n, n + 3, n + 1, n + 4, n + 2, n + 6, n + 5).reshape(*batch, rt * 16, nc * 128)
+    q = q.permute(*range(n), n, n + 2, n + 1, n + 4, n + 3, n + 6, n + 5).reshape(*batch, rt * 16, nc * 128)
     q = q[..., :K, :C].float()
     ng = _groups(C, group)
 
@@ -280,10 +280,10 @@ def work(case):
 def _exact_matrix(codes, scales, zeros, K, C, group):
     """One matrix in 64 bits, code by code from its place in the packed form."""
     rt, nc = codes.shape[0], codes.shape[1]
-    words = codes.contiguous().view(torch.int32).reshape(-1)               # [a][b][t][r][i]
+    words = codes.contiguous().view(torch.int32).reshape(-1)               # [a][b][r][t][i]
     row = torch.arange(K, device="cuda")[:, None]
     col = torch.arange(C, device="cuda")[None, :]
-    unit = (((row // 16) * nc + col // 128) * 4 + col // 8 % 4) * 16 + row % 16
+    unit = (((row // 16) * nc + col // 128) * 16 + row % 16) * 4 + col // 8 % 4
     e = col % 8
     shift = 4 * (e // 2 + 4 * (e % 2))
     q = (words[unit * 4 + col // 32 % 4] >> shift) & 15
