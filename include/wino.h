@@ -283,6 +283,88 @@ int wino_direct_conv_forward(const wino_direct_desc_t* desc, const int8_t* x_NHW
  * and clears the word. */
 int wino_direct_last_status(void* stream);
 
+/* ---- Layers with 4-bit weights and one scale per group of inputs --------------------------
+ * Quantized matrix products beside the convolutions: the classifier behind a convolutional body,
+ * the linear layers and the mixture-of-experts layers of a language model.  (The paper has no
+ * counterpart; its quantizer, Section 5.1, with a scale and a zero point for every `group`
+ * consecutive inputs of an output in place of one scale per layer.)
+ *
+ * Arithmetic.  A weight is (code - zero) * scale, code 0..15.  Products of codes less zeros with the
+ * inputs are exact and summed in 32-bit floats, a group's sum is multiplied by its scale, groups are
+ * summed in 32-bit floats, and the result is rounded once, to the output's type.
+ *
+ * Packed form (wino_packed_t), K outputs, C inputs, tiles of 16 outputs x 128 inputs:
+ *   codes   uint8 [K/16][C/128][16][4][16] (K, C rounded up): the 16 bytes at [a][b][r][t] hold row
+ *           16 a + r, inputs 128 b + 32 i + 8 t + e (i = 0..3, e = 0..7): little-endian 32-bit word i,
+ *           code of e in nibble e / 2 (e even) or 4 + e / 2 (e odd).  A tile is 1024 consecutive bytes.
+ *   scales  bf16 or fp16 [K/16][groups][16], groups = C / group rounded up
+ *   zeros   uint8 [K/16][groups][16], 0..15, or NULL: every zero is 8
+ * What stands in the codes of rows beyond K and inputs beyond C does not matter. */
+
+/* Element types of the layers below: 0 and 1 as out_dtype everywhere else. */
+enum { WINO_INT8 = 0, WINO_FLOAT = 1, WINO_BF16 = 2, WINO_FP16 = 3 };
+
+/* Packed weights; DEVICE pointers, 16-byte aligned.  group: 32, 64 or a multiple of 128 (one of at
+ * least C: one scale per output).  scale_dtype: WINO_BF16 or WINO_FP16. */
+typedef struct {
+  int32_t K, C, group, scale_dtype;
+  const void* codes_dev;
+  const void* scales_dev;
+  const uint8_t* zeros_dev; /* may be NULL */
+} wino_packed_t;
+
+/* Bytes of the codes, and number of scales (and of zeros); 0 for sizes that are not supported. */
+size_t wino_packed_code_bytes(int32_t K, int32_t C);
+size_t wino_packed_scale_count(int32_t K, int32_t C, int32_t group);
+
+/* Quantizes w [K][C] (w_dtype WINO_FLOAT, WINO_BF16 or WINO_FP16, rows w_stride >= C elements apart) into
+ * the buffers of `out`, which are written.  Without zeros, per group:
+ *   scale = round(max|w| / 7), zero = 8;  with zeros: lo = min(w, 0), hi = max(w, 0),
+ *   scale = round((hi - lo) / 15), zero = clamp(rne(-lo / scale), 0, 15);
+ *   code = clamp(rne(w / scale) + zero, 0, 15)
+ * in 32-bit floats, scales rounded to scale_dtype and at most its largest value; where the scale is 0, zero = code = 8.
+ * Rows beyond K get scale 0, zero 8, code 8.  w has to be finite (else: codes and scales without meaning).
+ * values_dev (nullable): dense [K][C] of w's type, the values that the codes stand for, rounded once. */
+int wino_quantize_weights(const wino_packed_t* out, const void* w_dev, int32_t w_dtype, int64_t w_stride,
+                          void* values_dev, void* stream);
+
+/* y = (x - z_x) s_x W^T + bias.  x [M][C], rows x_stride elements apart, of x_dtype; q_x (scale, zero
+ * point) is read for WINO_INT8 only.  y [M][K], rows y_stride elements apart, of y_dtype; for WINO_INT8
+ * through q_Y as everywhere in this library: Q(fmaf(sum, s_x/s_Y, bias/s_Y); 1).  Rows of x and y need the
+ * alignment of their elements only (16 bytes and multiples of 16 are faster).  M = 0 is no work.
+ * Elements of y between rows are left as they are. */
+typedef struct {
+  int32_t M, x_dtype, y_dtype;
+  int64_t x_stride, y_stride;
+  wino_quant_t q_x, q_Y;
+  wino_packed_t w;
+} wino_linear_desc_t;
+int wino_linear_forward(const wino_linear_desc_t* desc, const void* x_dev, const float* bias_K_dev, void* y_dev,
+                        void* stream);
+
+/* Mixture of experts for T tokens of D values:
+ *   l = x R^T + r;  p = softmax(l);  S = the top_k largest of l (equal ones: the lowest index first);
+ *   a_e = p_e, or p_e / sum of S where `normalize`;
+ *   y = sum over e in S of a_e down_e(silu(gate_e(x)) * up_e(x)),  silu(v) = v / (1 + exp(-v)).
+ * dtype (x, R, y): WINO_FLOAT, WINO_BF16 or WINO_FP16.  gate, up: K = I, C = D; down: K = D, C = I; each E
+ * matrices in a row (codes wino_packed_code_bytes, scales and zeros wino_packed_scale_count apart).
+ * router [E][D] dense; router_bias float [E] or NULL, -inf takes an expert out.  A token whose every expert
+ * is out gets ids 0 .. top_k-1, weights 0 and y = 0; where it has fewer than top_k experts left, the rest of its
+ * ids are the lowest experts that are out, with weight 0.  A NaN or +inf among a token's logits makes its weights and y NaN.
+ * ids int32 [T][top_k] and weights float [T][top_k] receive S, largest first, and a.
+ * E <= 512, top_k <= 16.  Any T; the layer is laid out for few tokens (up to 64 go through the experts at
+ * once, and an expert's weights are read once for up to 16 of its tokens).  T = 0 is no work.
+ * workspace_dev: wino_experts_workspace_bytes, 16-byte aligned, not shared by calls that may overlap. */
+typedef struct {
+  int32_t T, D, I, E, top_k, normalize, dtype;
+  int64_t x_stride, y_stride;
+  wino_packed_t gate, up, down;
+} wino_experts_desc_t;
+size_t wino_experts_workspace_bytes(const wino_experts_desc_t* desc);
+int wino_experts_forward(const wino_experts_desc_t* desc, const void* x_dev, const void* router_dev,
+                         const float* router_bias_dev, void* y_dev, int32_t* ids_dev, float* weights_dev,
+                         void* workspace_dev, void* stream);
+
 /* Synchronizes `stream` and returns the plan's device status word: WINO_OK, or
  * WINO_ERR_TIMEOUT if a bounded wait inside a kernel expired (the kernel then
  * stopped early and its output is undefined), or WINO_ERR_CUDA.  On the device

@@ -33,8 +33,12 @@ EXPORTS = [
     "wino_direct_conv_forward", "wino_direct_last_status", "wino_last_status", "wino_debug_dump_stage",
     "wino_debug_forward_accumulators", "wino_debug_run_stages", "wino_debug_mma_probe",
     "wino_debug_wait_probe", "wino_debug_once_per_device", "wino_launch_count", "wino_destroy",
-    "wino_strerror",
+    "wino_strerror", "wino_packed_code_bytes", "wino_packed_scale_count", "wino_quantize_weights",
+    "wino_linear_forward", "wino_experts_workspace_bytes", "wino_experts_forward",
 ]
+
+# element types of the layers with 4-bit weights (0 and 1 as out_dtype elsewhere)
+INT8, FLOAT, BF16, FP16 = 0, 1, 2, 3
 
 
 class QuantC(ct.Structure):
@@ -49,6 +53,22 @@ class DescC(ct.Structure):
                 ("transforms_exact", ct.c_int32),
                 ("q_x", QuantC), ("q_w", QuantC), ("q_V", QuantC), ("q_U", QuantC),
                 ("q_M", QuantC), ("q_Y", QuantC), ("out_dtype", ct.c_int32)]
+
+
+class PackedC(ct.Structure):
+    _fields_ = [("K", ct.c_int32), ("C", ct.c_int32), ("group", ct.c_int32), ("scale_dtype", ct.c_int32),
+                ("codes_dev", ct.c_void_p), ("scales_dev", ct.c_void_p), ("zeros_dev", ct.c_void_p)]
+
+
+class LinearDescC(ct.Structure):
+    _fields_ = [("M", ct.c_int32), ("x_dtype", ct.c_int32), ("y_dtype", ct.c_int32),
+                ("x_stride", ct.c_int64), ("y_stride", ct.c_int64), ("q_x", QuantC), ("q_Y", QuantC), ("w", PackedC)]
+
+
+class ExpertsDescC(ct.Structure):
+    _fields_ = [("T", ct.c_int32), ("D", ct.c_int32), ("I", ct.c_int32), ("E", ct.c_int32), ("top_k", ct.c_int32),
+                ("normalize", ct.c_int32), ("dtype", ct.c_int32), ("x_stride", ct.c_int64), ("y_stride", ct.c_int64),
+                ("gate", PackedC), ("up", PackedC), ("down", PackedC)]
 
 
 class WinoError(RuntimeError):
@@ -89,6 +109,15 @@ def _load() -> ct.CDLL:
     lib.wino_destroy.restype = None
     lib.wino_strerror.argtypes = [i32]
     lib.wino_strerror.restype = ct.c_char_p
+    lib.wino_packed_code_bytes.argtypes = [ct.c_int32, ct.c_int32]
+    lib.wino_packed_code_bytes.restype = sz
+    lib.wino_packed_scale_count.argtypes = [ct.c_int32, ct.c_int32, ct.c_int32]
+    lib.wino_packed_scale_count.restype = sz
+    lib.wino_quantize_weights.argtypes = [ct.POINTER(PackedC), vp, ct.c_int32, ct.c_int64, vp, vp]
+    lib.wino_linear_forward.argtypes = [ct.POINTER(LinearDescC), vp, vp, vp, vp]
+    lib.wino_experts_workspace_bytes.argtypes = [ct.POINTER(ExpertsDescC)]
+    lib.wino_experts_workspace_bytes.restype = sz
+    lib.wino_experts_forward.argtypes = [ct.POINTER(ExpertsDescC), vp, vp, vp, vp, vp, vp, vp, vp]
     return lib
 
 
@@ -145,6 +174,50 @@ def direct_conv_forward(N, C, H, W, K, stride, q_x, q_w, q_Y, x_dev, w_dev, bias
                                      out_dtype, stream, s_w_K_dev, s_Y_K_dev)
     if rc != WINO_OK:
         raise WinoError(rc, "wino_direct_conv_forward")
+
+
+# --- layers with 4-bit weights: the C entry points on addresses (layer.py has them on tensors) ---
+def packed_code_bytes(K: int, C: int) -> int:
+    return _lib.wino_packed_code_bytes(K, C)
+
+
+def packed_scale_count(K: int, C: int, group: int) -> int:
+    return _lib.wino_packed_scale_count(K, C, group)
+
+
+def packed(K, C, group, scale_dtype, codes_dev, scales_dev, zeros_dev=None) -> PackedC:
+    return PackedC(K, C, group, scale_dtype, _dptr(codes_dev), _dptr(scales_dev), _dptr(zeros_dev))
+
+
+def quantize_weights(out: PackedC, w_dev, w_dtype, w_stride, values_dev=None, stream=None) -> None:
+    """wino_quantize_weights: weights to 4-bit codes, scales and (where `out` has them) zeros."""
+    _check(_lib.wino_quantize_weights(ct.byref(out), _dptr(w_dev), w_dtype, w_stride, _dptr(values_dev),
+                                      _stream_handle(stream)), "wino_quantize_weights")
+
+
+def linear_forward(M, x_dtype, y_dtype, x_stride, y_stride, w: PackedC, x_dev, bias_dev, y_dev, q_x=None, q_Y=None,
+                   stream=None) -> None:
+    """wino_linear_forward: y = x W^T + bias with 4-bit weights."""
+    d = LinearDescC(M, x_dtype, y_dtype, x_stride, y_stride, _quant(q_x or {}), _quant(q_Y or {}), w)
+    _check(_lib.wino_linear_forward(ct.byref(d), _dptr(x_dev), _dptr(bias_dev), _dptr(y_dev),
+                                    _stream_handle(stream)), "wino_linear_forward")
+
+
+def experts_desc(T, D, I, E, top_k, dtype, x_stride, y_stride, gate: PackedC, up: PackedC, down: PackedC,
+                 normalize=True) -> ExpertsDescC:
+    return ExpertsDescC(T, D, I, E, top_k, int(normalize), dtype, x_stride, y_stride, gate, up, down)
+
+
+def experts_workspace_bytes(desc: ExpertsDescC) -> int:
+    return _lib.wino_experts_workspace_bytes(ct.byref(desc))
+
+
+def experts_forward(desc: ExpertsDescC, x_dev, router_dev, router_bias_dev, y_dev, ids_dev, weights_dev, workspace_dev,
+                    stream=None) -> None:
+    """wino_experts_forward: a mixture-of-experts layer for a few tokens."""
+    _check(_lib.wino_experts_forward(ct.byref(desc), _dptr(x_dev), _dptr(router_dev), _dptr(router_bias_dev),
+                                     _dptr(y_dev), _dptr(ids_dev), _dptr(weights_dev), _dptr(workspace_dev),
+                                     _stream_handle(stream)), "wino_experts_forward")
 
 
 class Plan:

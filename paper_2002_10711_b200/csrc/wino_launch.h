@@ -8,6 +8,7 @@
 
 #include <cuda.h>
 #include <cuda_runtime.h>
+#include "wino.h"
 #include "wino_common.cuh"
 
 namespace wino {
@@ -232,6 +233,15 @@ int launch_mma_peak(int iters, int num_sms, int device, int* status, cudaStream_
 // Bounded-wait probe: one block waits, with the given cycle limit, on a barrier
 // that nothing arrives at, records WINO_ERR_TIMEOUT in *status and exits normally.
 int launch_wait_probe(long long limit_cycles, int* status, cudaStream_t st);
+
+// Layers with 4-bit weights (wino_packed_host.cu checks the arguments).
+int launch_quantize(const wino_packed_t& out, const void* w, int w_dtype, int64_t w_stride, void* values,
+                    cudaStream_t st);
+int launch_linear(const wino_linear_desc_t& d, const void* x, const float* bias, void* y, int num_sms,
+                  cudaStream_t st);
+size_t experts_workspace(int T, int I, int top_k, int dtype);
+int launch_experts(const wino_experts_desc_t& d, const void* x, const void* router, const float* router_bias, void* y,
+                   int* ids, float* weights, void* workspace, int num_sms, cudaStream_t st);
 
 enum { kOutMq = 0, kOutI32 = 1 };
 constexpr int kBM = 128;      // tiles per GEMM block (MMA M)

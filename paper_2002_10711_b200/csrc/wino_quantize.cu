@@ -1,0 +1,206 @@
+// Weights [K][C] -> 4-bit codes, scales and zeros of groups of inputs (and the values the codes stand for).
+//
+// Bound by memory: w is read once, codes, scales and values written once.  A warp takes 8 outputs x 128
+// inputs; lane (g, t) holds of output g the 32 inputs of its 16-byte unit of codes, so that a group's
+// extremes are those of four lanes and a unit leaves in one store.  A group longer than 128 inputs is read
+// twice, by the same warp one after the other.
+#include "wino_packed.cuh"
+
+namespace wino {
+
+struct QuantizeArgs {
+  uint4* codes;
+  uint16_t* scales;
+  uint8_t* zeros;
+  const char* w;
+  char* values;
+  long w_row;           // bytes
+  int K, C, group, tiles_C, groups, scale_f16, vec, vec_values;
+};
+
+constexpr int kQuantWarps = 4;
+
+template <int DT>
+__device__ __forceinline__ void load_weights(const QuantizeArgs& a, const char* row, int k, float (&v)[8]) {
+  to_floats<DT>(load_input<DT>(row, k, a.C, a.vec, 0), v);
+}
+
+template <int DT>
+__device__ __forceinline__ void store_values(const QuantizeArgs& a, char* row, int k, const float (&v)[8]) {
+  if constexpr (DT == WINO_FLOAT) {
+    float* p = reinterpret_cast<float*>(row) + k;
+    if (a.vec_values && k + 8 <= a.C) {
+      reinterpret_cast<float4*>(p)[0] = make_float4(v[0], v[1], v[2], v[3]);
+      reinterpret_cast<float4*>(p)[1] = make_float4(v[4], v[5], v[6], v[7]);
+    } else {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) if (k + e < a.C) p[e] = v[e];
+    }
+  } else {
+    uint16_t h[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+      h[e] = DT == WINO_FP16 ? __half_as_ushort(__float2half_rn(v[e])) : __bfloat16_as_ushort(__float2bfloat16_rn(v[e]));
+    uint16_t* p = reinterpret_cast<uint16_t*>(row) + k;
+    if (a.vec_values && k + 8 <= a.C) {
+      *reinterpret_cast<uint4*>(p) = make_uint4(h[0] | (uint32_t)h[1] << 16, h[2] | (uint32_t)h[3] << 16,
+                                                h[4] | (uint32_t)h[5] << 16, h[6] | (uint32_t)h[7] << 16);
+    } else {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) if (k + e < a.C) p[e] = h[e];
+    }
+  }
+}
+
+struct Range {
+  float lo, hi;   // min(w, 0), max(w, 0)
+  __device__ __forceinline__ void join(float v) { lo = fminf(lo, v); hi = fmaxf(hi, v); }
+  __device__ __forceinline__ void join(const Range& r) { lo = fminf(lo, r.lo); hi = fmaxf(hi, r.hi); }
+  // over the four lanes of a row
+  __device__ __forceinline__ void join_lanes() {
+#pragma unroll
+    for (int o = 1; o < 4; o *= 2) {
+      lo = fminf(lo, __shfl_xor_sync(0xffffffffu, lo, o));
+      hi = fmaxf(hi, __shfl_xor_sync(0xffffffffu, hi, o));
+    }
+  }
+};
+
+struct Grid { float s, z; uint16_t bits; };
+__device__ __forceinline__ Grid grid_of(const QuantizeArgs& a, const Range& r) {
+  Grid q;
+  const float span = a.zeros ? __fdiv_rn(__fsub_rn(r.hi, r.lo), 15.0f) : __fdiv_rn(fmaxf(r.hi, -r.lo), 7.0f);
+  if (a.scale_f16) {
+    q.bits = __half_as_ushort(__float2half_rn(fminf(span, 65504.0f)));
+  } else {
+    q.bits = __bfloat16_as_ushort(__float2bfloat16_rn(fminf(span, __uint_as_float(0x7F7F0000u))));
+  }
+  q.s = scale_to_float(q.bits, a.scale_f16);
+  q.z = a.zeros && q.s > 0.0f ? fminf(fmaxf(rintf(__fdiv_rn(-r.lo, q.s)), 0.0f), 15.0f) : 8.0f;
+  return q;
+}
+
+template <int DT>
+__device__ __forceinline__ uint32_t codes_of(const QuantizeArgs& a, const Grid& q, const float (&v)[8], char* out, int k) {
+  uint32_t word = 0;
+  float back[8];
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    const float c = q.s > 0.0f ? fminf(fmaxf(__fadd_rn(rintf(__fdiv_rn(v[e], q.s)), q.z), 0.0f), 15.0f) : q.z;
+    back[e] = __fmul_rn(__fsub_rn(c, q.z), q.s);
+    word |= (uint32_t)(int)c << (4 * (e / 2 + 4 * (e & 1)));
+  }
+  if (out != nullptr) store_values<DT>(a, out, k, back);
+  return word;
+}
+
+// grid.x: warps over (pairs of half tiles of outputs) x parts of the inputs; span: tiles of inputs that a
+// warp takes, whole groups
+template <int DT>
+__global__ void __launch_bounds__(kQuantWarps * 32)
+k_quantize(const __grid_constant__ QuantizeArgs a, int span, int parts) {
+  const int lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
+  const long unit = blockIdx.x * (long)kQuantWarps + (threadIdx.x >> 5);
+  const long half = unit / parts;                 // 8 outputs
+  const int first = (int)(unit - half * parts) * span;
+  griddep_launch();
+  griddep_wait();
+  if (half >= 2l * ((a.K + 15) / 16)) return;
+  const long k = half * 8 + g;                    // output
+  const bool in = k < a.K;
+  const char* row = a.w + (in ? k : 0) * a.w_row;
+  char* out = a.values != nullptr && in ? a.values + k * (long)a.C * Input<DT>::kBytes : nullptr;
+  const long tile_K = half >> 1;
+  uint4* codes = a.codes + tile_K * a.tiles_C * 64 + (half & 1) * 32 + lane;
+  const long group_at = tile_K * a.groups * 16 + (half & 1) * 8 + g;
+  const int last = min(first + span, a.tiles_C);
+  auto put = [&](int grp, const Grid& q) {
+    if (t == 0 && grp < a.groups) {
+      a.scales[group_at + grp * 16l] = in ? q.bits : (uint16_t)0;
+      if (a.zeros) a.zeros[group_at + grp * 16l] = in ? (uint8_t)(int)q.z : (uint8_t)8;
+    }
+  };
+  if (a.group <= 128) {
+    const int per = a.group / 32;                 // MMA pairs (32 inputs) a group
+    for (int c = first; c < last; ++c) {
+      float v[4][8];
+      Range r[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) load_weights<DT>(a, row, c * 128 + 32 * i + 8 * t, v[i]);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        r[i].lo = r[i].hi = 0.0f;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) r[i].join(v[i][e]);
+      }
+      if (per >= 2) { r[0].join(r[1]); r[2].join(r[3]); }
+      if (per == 4) r[0].join(r[2]);
+      uint32_t word[4];
+      Grid q;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        if (i % per == 0) {
+          r[i].join_lanes();
+          q = grid_of(a, r[i]);
+          put(c * (4 / per) + i / per, q);
+        }
+        if (!in) q.s = 0.0f, q.z = 8.0f;
+        word[i] = codes_of<DT>(a, q, v[i], out, c * 128 + 32 * i + 8 * t);
+      }
+      codes[c * 64l] = make_uint4(word[0], word[1], word[2], word[3]);
+    }
+    return;
+  }
+  const int per = a.group / 128;                  // tiles a group; span is a multiple of it
+  for (int c0 = first; c0 < last; c0 += per) {
+    const int c1 = min(c0 + per, last);
+    Range r;
+    r.lo = r.hi = 0.0f;
+    for (int c = c0; c < c1; ++c)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        float v[8];
+        load_weights<DT>(a, row, c * 128 + 32 * i + 8 * t, v);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) r.join(v[e]);
+      }
+    r.join_lanes();
+    Grid q = grid_of(a, r);
+    put(c0 / per, q);
+    if (!in) q.s = 0.0f, q.z = 8.0f;
+    for (int c = c0; c < c1; ++c) {
+      uint32_t word[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        float v[8];
+        load_weights<DT>(a, row, c * 128 + 32 * i + 8 * t, v);
+        word[i] = codes_of<DT>(a, q, v, out, c * 128 + 32 * i + 8 * t);
+      }
+      codes[c * 64l] = make_uint4(word[0], word[1], word[2], word[3]);
+    }
+  }
+}
+
+int launch_quantize(const wino_packed_t& o, const void* w, int w_dtype, int64_t w_stride, void* values,
+                    cudaStream_t st) {
+  QuantizeArgs a;
+  a.codes = (uint4*)const_cast<void*>(o.codes_dev);
+  a.scales = (uint16_t*)const_cast<void*>(o.scales_dev);
+  a.zeros = const_cast<uint8_t*>(o.zeros_dev);
+  const int size = w_dtype == WINO_FLOAT ? 4 : 2;
+  a.w = (const char*)w; a.w_row = (long)w_stride * size; a.values = (char*)values;
+  a.K = o.K; a.C = o.C; a.group = o.group; a.tiles_C = (o.C + 127) / 128;
+  a.groups = (o.C + o.group - 1) / o.group; a.scale_f16 = o.scale_dtype == WINO_FP16;
+  a.vec = reinterpret_cast<uintptr_t>(w) % 16 == 0 && a.w_row % 16 == 0;
+  a.vec_values = reinterpret_cast<uintptr_t>(values) % 16 == 0 && ((long)o.C * size) % 16 == 0;
+  const long halves = 2l * ((o.K + 15) / 16);
+  const int per = o.group <= 128 ? 1 : (int)((o.group + 127l) / 128 < a.tiles_C ? o.group / 128 : a.tiles_C);
+  const int span = per, parts = (a.tiles_C + span - 1) / span;
+  const long blocks = (halves * parts + kQuantWarps - 1) / kQuantWarps;
+  if (blocks > 0x7fffffffl) return WINO_ERR_UNSUPPORTED;
+  auto kernel = w_dtype == WINO_FLOAT ? k_quantize<WINO_FLOAT> : w_dtype == WINO_BF16 ? k_quantize<WINO_BF16>
+                                                                                       : k_quantize<WINO_FP16>;
+  return launch_kernel(kernel, dim3((unsigned)blocks), dim3(kQuantWarps * 32), 0, st, true, a, span, parts);
+}
+
+}  // namespace wino

@@ -1,9 +1,11 @@
-"""Convenience wrapper: one Winograd-aware quantized conv layer on the GPU.
-
-Holds a Plan plus the device buffers it needs (transformed weights, workspace).
+"""Convenience wrappers on torch tensors: one Winograd-aware quantized conv layer (a Plan plus the
+device buffers it needs: transformed weights, workspace), and the layers with 4-bit weights and
+group scales: linear_w4, experts_w4, and quantize_w4 for their weights.
 All arithmetic happens in the CUDA library; torch only owns memory and streams.
 """
 from __future__ import annotations
+
+from typing import NamedTuple, Optional
 
 import numpy as np
 import torch
@@ -158,3 +160,100 @@ def calibrate_per_channel(make_plan, x_q, w_q, bias, s_x: float, s_w_K, output_p
     if output_per_channel:
         return s_V, s_U_K, s_M_K, scales(y.abs().amax(dim=(0, 1, 2)).cpu().numpy())
     return s_V, s_U_K, s_M_K, scale(float(y.abs().max()))
+
+
+# --- layers with 4-bit weights -----------------------------------------------------------
+class W4(NamedTuple):
+    """A weight matrix [K, C], or a batch of them, as 4-bit codes with one scale per `group` inputs of an
+    output.  codes uint8 [..., K/16, C/128, 16, 4, 16] (K and C rounded up; the layout is wino_packed_t's),
+    scales bfloat16 or float16 [..., K/16, groups, 16], zeros uint8 like scales, or None (every zero is 8).
+    The functions below take any tuple of these six."""
+    codes: torch.Tensor
+    scales: torch.Tensor
+    zeros: Optional[torch.Tensor]
+    K: int
+    C: int
+    group: int
+
+
+def _w4_result(r, what: str):
+    if type(r) is int:
+        raise binding.WinoError(r, what)
+    return r
+
+
+def quantize_w4(weight: torch.Tensor, group: int = 128, symmetric: bool = True, scale_dtype=torch.bfloat16,
+                values: bool = False):
+    """4-bit codes of `weight` ([K, C] or [E, K, C]; float32, bfloat16 or float16, on the GPU), with a scale,
+    and unless `symmetric` a zero, for every `group` consecutive inputs (32, 64 or a multiple of 128).  The
+    rules are wino_quantize_weights'.  Returns a W4; with values=True also the values that the codes stand
+    for, in the weights' type (what quantization-aware training puts in the weights' place)."""
+    codes, scales, zeros, K, C, back = _w4_result(
+        _native_torch.quantize_w4(weight, group, symmetric, scale_dtype, values), "wino_quantize_weights")
+    w = W4(codes, scales, zeros, K, C, group)
+    return (w, back) if values else w
+
+
+def linear_w4(x: torch.Tensor, w, bias: Optional[torch.Tensor] = None, q_x=None, q_Y=None, out_dtype=None,
+              out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """x [..., C] times the transpose of w (W4) plus bias (float32 [K]): [..., K].
+
+    x is float32, bfloat16 or float16, or int8 codes with their quantizer q_x (scale, zero_point), as a
+    convolution of this package leaves them.  The result has x's type (float32 for codes), `out_dtype`, or
+    with q_Y int8 codes.  out: a tensor to write to, whose rows may be strided.  Made for few rows; forward
+    only (inputs that ask for a gradient are refused).  Runs on the current stream of x's device."""
+    return _w4_result(_native_torch.linear_w4(x, w, bias, q_x, q_Y, out_dtype, out), "wino_linear_forward")
+
+
+def experts_w4(x: torch.Tensor, router: torch.Tensor, gate, up, down, top_k: int,
+               router_bias: Optional[torch.Tensor] = None, normalize: bool = True,
+               out: Optional[torch.Tensor] = None):
+    """A mixture-of-experts layer for a few tokens x [..., D]: softmax of x router^T + router_bias, the top_k
+    largest (ties: lowest index), and the sum over them of weight * down(silu(gate(x)) * up(x)).
+
+    router [E, D] has x's type (float32, bfloat16 or float16); gate and up are W4 batches [E, I, D], down
+    [E, D, I].  normalize: weights of a token add up to one.  router_bias float32 [E]: -inf takes an expert
+    out.  Returns (y [..., D] of x's type, ids int32 [..., top_k], weights float32 [..., top_k]).  Forward
+    only.  Runs on the current stream of x's device."""
+    return _w4_result(_native_torch.experts_w4(x, router, gate, up, down, top_k, router_bias, normalize, out),
+                      "wino_experts_forward")
+
+
+def _by_tiles(v: torch.Tensor, fill) -> torch.Tensor:
+    """[..., K, groups] -> [..., K/16, groups, 16]."""
+    K, groups = v.shape[-2:]
+    v = torch.nn.functional.pad(v, (0, 0, 0, -K % 16), value=fill)
+    return v.view(*v.shape[:-2], -1, 16, groups).transpose(-1, -2).contiguous()
+
+
+def pack_w4(codes: torch.Tensor, scales: torch.Tensor, zeros: Optional[torch.Tensor] = None, group: int = 128) -> W4:
+    """A W4 from codes 0..15 (any integer type) [..., K, C], scales (bfloat16 or float16) and zeros
+    [..., K, groups], as checkpoints hold them.  A rearrangement with torch, done once."""
+    *batch, K, C = codes.shape
+    groups = -(-C // group)
+    if scales.shape != (*batch, K, groups) or (zeros is not None and zeros.shape != scales.shape):
+        raise ValueError(f"scales and zeros must be [..., K, groups]: {(*batch, K, groups)}")
+    if scales.dtype not in (torch.bfloat16, torch.float16):
+        raise ValueError("scales must be bfloat16 or float16")
+    for v in (codes, zeros):
+        if v is not None and v.numel() and (int(v.min()) < 0 or int(v.max()) > 15):
+            raise ValueError("codes and zeros must be 0..15")
+    q = torch.nn.functional.pad(codes.to(torch.uint8), (0, -C % 128, 0, -K % 16))
+    tiles_K, tiles_C, n = q.shape[-2] // 16, q.shape[-1] // 128, len(batch)
+    q = q.view(*batch, tiles_K, 16, tiles_C, 4, 4, 4, 2)          # a r b i t (e / 2) (e % 2)
+    q = q.permute(*range(n), n, n + 2, n + 1, n + 4, n + 3, n + 6, n + 5).reshape(*batch, tiles_K, tiles_C, 16, 4, 16, 2)
+    return W4((q[..., 0] | q[..., 1] << 4).contiguous(), _by_tiles(scales, 0.0),
+              None if zeros is None else _by_tiles(zeros.to(torch.uint8), 8), K, C, group)
+
+
+def unpack_w4(w):
+    """(codes uint8 [..., K, C], scales [..., K, groups], zeros or None): pack_w4 backwards."""
+    codes, scales, zeros, K, C, group = w
+    *batch, tiles_K, tiles_C, _, _, _ = codes.shape
+    n = len(batch)
+    q = torch.stack((codes & 15, codes >> 4), -1).view(*batch, tiles_K, tiles_C, 16, 4, 4, 2, 4)   # a b r t i h e/2
+    q = q.permute(*range(n), n, n + 2, n + 1, n + 4, n + 3, n + 6, n + 5).reshape(*batch, tiles_K * 16, tiles_C * 128)
+
+    def rows(v):
+        return v.transpose(-1, -2).reshape(*batch, tiles_K * 16, v.shape[-2])[..., :K, :].contiguous()
+    return q[..., :K, :C].contiguous(), rows(scales), None if zeros is None else rows(zeros)
