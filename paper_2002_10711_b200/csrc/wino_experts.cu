@@ -3,12 +3,13 @@
 // Bound by reading the chosen experts' codes, each once.  Three launches, each starting while the one in
 // front of it ends:
 //   route  a block per token: its logits, the top_k experts and their weights
-//   up     a block per (chosen expert, 16 of its inner values): gate and up products of up to 8 NT of the
-//          expert's tokens, h = weight * silu(gate) * up, kept as the sum of two bf16 (three for 32-bit
+//   up     a block per chosen expert and up to 8 row tiles of 16 of its inner values: gate and up products of up
+//          to 8 NT of the expert's tokens at a time, h = weight * silu(gate) * up, kept as the sum of two bf16 (three for 32-bit
 //          inputs), which the next product takes as it is: 16 (24) significant bits, so that nothing
 //          is rounded to the output's type in between
-//   down   a block (or cluster) per 16 outputs: the products of every chosen expert, summed over experts in
-//          their order; warps share the 1 KB tiles of all experts
+//   down   a block (or cluster) per up to 8 row tiles of outputs: the products of every chosen expert, summed
+//          over experts in their order; the warps of a row tile share the tiles of all experts
+// Warps stream their tiles through rings of asynchronous copies, as in the linear layer.
 // A token chooses an expert at most once, so that an expert's tokens are a set of bits, which every block
 // makes for itself from the ids: no counters, no atomics on global memory, sums in a fixed order.
 #include <cooperative_groups.h>
@@ -19,7 +20,7 @@ namespace wino {
 
 namespace cg = cooperative_groups;
 
-constexpr int kMaxExperts = 512, kSliceTokens = 64;
+constexpr int kMaxExperts = 512, kMaxTopK = 16, kSliceTokens = 64;
 constexpr int kExpertWarps = 8;
 
 struct ExpertsArgs {
@@ -47,99 +48,145 @@ __device__ __forceinline__ Packed expert_of(Packed w, int e, long units, long sc
 }
 
 // ---- router -----------------------------------------------------------------------------
-constexpr int kRouteThreads = 512;
+// A cluster per token: each block the logits of its share of the experts, a warp at a time; the first
+// block ranks them all: an expert's place is the number of experts in front of it.
+constexpr int kRouteThreads = 256;
 template <int DT>
 __global__ void __launch_bounds__(kRouteThreads)
 k_experts_route(const __grid_constant__ ExpertsArgs a) {
-  __shared__ float logits[kMaxExperts];
-  const int token = blockIdx.x, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  using In = Input<DT>;
+  __shared__ __align__(16) float logits[kMaxExperts];
+  __shared__ float top_l[kMaxTopK];
+  __shared__ int top_e[kMaxTopK];
+  const cg::cluster_group cluster = cg::this_cluster();
+  const int S = (int)cluster.num_blocks(), rank = (int)cluster.block_rank();
+  const int token = blockIdx.x / S, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   griddep_launch();
+  for (int e = threadIdx.x; e < kMaxExperts; e += kRouteThreads) logits[e] = -INFINITY;   // behind the last: for four at a time
+  cluster.sync();
   griddep_wait();
   const char* x = a.x + token * a.x_row;
-  for (int e = warp; e < a.E; e += kRouteThreads / 32) {
-    const char* r = a.router + (long)e * a.D * Input<DT>::kBytes;
+  float* to = cluster.map_shared_rank(logits, 0);
+  for (int e = rank + S * warp; e < a.E; e += S * (kRouteThreads / 32)) {
+    const char* r = a.router + (long)e * a.D * In::kBytes;
     float s = 0.0f;
-    for (int k = lane * 8; k < a.D; k += 256) {
+    auto add = [&](const In& xi, const In& ri) {
       float xv[8], rv[8];
-      to_floats<DT>(load_input<DT>(x, k, a.D, a.vec, 0), xv);
-      to_floats<DT>(load_input<DT>(r, k, a.D, a.vec_router, 0), rv);
+      to_floats<DT>(xi, xv);
+      to_floats<DT>(ri, rv);
 #pragma unroll
       for (int i = 0; i < 8; ++i) s = __fmaf_rn(xv[i], rv[i], s);
-    }
+    };
+    int k = lane * 8;
+    if (a.vec && a.vec_router)
+      for (; k + 3 * 256 + 8 <= a.D; k += 4 * 256) {
+        In xi[4], ri[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          xi[i].load(x + (k + 256 * i) * In::kBytes);
+          ri[i].load(r + (k + 256 * i) * In::kBytes);
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) add(xi[i], ri[i]);
+      }
+    for (; k < a.D; k += 256) add(load_input<DT>(x, k, a.D, a.vec, 0), load_input<DT>(r, k, a.D, a.vec_router, 0));
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) s = __fadd_rn(s, __shfl_xor_sync(0xffffffffu, s, o));
-    if (lane == 0) logits[e] = a.router_bias ? __fadd_rn(s, __ldg(a.router_bias + e)) : s;
+    if (lane == 0) to[e] = a.router_bias ? __fadd_rn(s, a.router_bias[e]) : s;
+  }
+  cluster.sync();
+  if (rank != 0) return;
+  bool odd = false;                       // NaN or +inf
+  for (int e = threadIdx.x; e < a.E; e += kRouteThreads) odd |= !(logits[e] < INFINITY);
+  odd = __syncthreads_or(odd);
+  // `by` neighbouring lanes count for one expert
+  int by = 1;
+  while (by < 32 && a.E * by * 2 <= kRouteThreads) by *= 2;
+  for (int e0 = 0; e0 < a.E; e0 += kRouteThreads / by) {
+    const int e = e0 + threadIdx.x / by, part = threadIdx.x % by;
+    const float l = e < a.E ? logits[e] : 0.0f;
+    int place = 0;
+    for (int f = part * 4; f < a.E; f += by * 4) {
+      const float4 o = *reinterpret_cast<const float4*>(logits + f);
+      place += o.x > l || (o.x == l && f < e);
+      place += o.y > l || (o.y == l && f + 1 < e);
+      place += o.z > l || (o.z == l && f + 2 < e);
+      place += o.w > l || (o.w == l && f + 3 < e);
+    }
+    for (int o = 1; o < by; o *= 2) place += __shfl_xor_sync(0xffffffffu, place, o);
+    if (part == 0 && e < a.E && place < a.top_k && !odd) top_l[place] = l, top_e[place] = e;
   }
   __syncthreads();
   if (warp != 0) return;
-  constexpr int kPer = kMaxExperts / 32;
-  float v[kPer];          // experts 32 i + lane
-  float top = -INFINITY;
-  bool nan = false;
-#pragma unroll
-  for (int i = 0; i < kPer; ++i) {
-    const int e = 32 * i + lane;
-    v[i] = e < a.E ? logits[e] : -INFINITY;
-    nan |= !(v[i] < INFINITY);       // NaN or +inf
-    top = fmaxf(top, v[i]);
+  const bool mine = lane < a.top_k;
+  if (odd) {
+    if (mine) {
+      a.ids[(long)token * a.top_k + lane] = lane;
+      a.weights[(long)token * a.top_k + lane] = __uint_as_float(0x7FC00000u);
+    }
+    return;
   }
-  nan = __any_sync(0xffffffffu, nan);
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
-  float sum = 0.0f;
+  const float top = top_l[0];
+  auto share = [&](float l) { return l > -INFINITY ? expf(__fsub_rn(l, top)) : 0.0f; };
+  const float p = mine ? share(top_l[lane]) : 0.0f;
+  float sum = p;
   if (!a.normalize) {
-#pragma unroll
-    for (int i = 0; i < kPer; ++i) sum = __fadd_rn(sum, v[i] > -INFINITY ? expf(__fsub_rn(v[i], top)) : 0.0f);
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) sum = __fadd_rn(sum, __shfl_xor_sync(0xffffffffu, sum, o));
+    sum = 0.0f;
+    for (int e = lane; e < a.E; e += 32) sum = __fadd_rn(sum, share(logits[e]));
   }
-  // lane j keeps the j-th choice; `taken`: this lane's experts that are chosen already
-  uint32_t taken = 0;
-  int my_id = 0;
-  float my_l = -INFINITY;
-  for (int j = 0; j < a.top_k; ++j) {
-    float best = -INFINITY;
-    int at = kMaxExperts;
 #pragma unroll
-    for (int i = 0; i < kPer; ++i) {
-      const int e = 32 * i + lane;
-      if (e < a.E && !(taken >> i & 1) && (at == kMaxExperts || v[i] > best)) best = v[i], at = e;
-    }
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) {
-      const float b = __shfl_xor_sync(0xffffffffu, best, o);
-      const int n = __shfl_xor_sync(0xffffffffu, at, o);
-      if (n < kMaxExperts && (at == kMaxExperts || b > best || (b == best && n < at))) best = b, at = n;
-    }
-    if (nan) at = j;
-    if ((at & 31) == lane) taken |= 1u << (at >> 5);
-    if (lane == j) my_id = at, my_l = best;
-  }
-  float p = lane < a.top_k && my_l > -INFINITY ? expf(__fsub_rn(my_l, top)) : 0.0f;
-  if (a.normalize) {
-    sum = p;
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) sum = __fadd_rn(sum, __shfl_xor_sync(0xffffffffu, sum, o));
-  }
-  if (lane < a.top_k) {
-    a.ids[(long)token * a.top_k + lane] = my_id;
-    a.weights[(long)token * a.top_k + lane] = nan ? __uint_as_float(0x7FC00000u) : p > 0.0f ? __fdiv_rn(p, sum) : 0.0f;
+  for (int o = 16; o > 0; o >>= 1) sum = __fadd_rn(sum, __shfl_xor_sync(0xffffffffu, sum, o));
+  if (mine) {
+    a.ids[(long)token * a.top_k + lane] = top_e[lane];
+    a.weights[(long)token * a.top_k + lane] = p > 0.0f ? __fdiv_rn(p, sum) : 0.0f;
   }
 }
 
 // ---- who goes where ---------------------------------------------------------------------
+// The chosen experts and their rows of h; pairs (token, expert) whose weight is 0 are left out.
 struct Lists {
   unsigned long long tokens[kMaxExperts];   // set of tokens of each expert
-  uint16_t expert[kMaxExperts + 1];         // chosen experts, ascending
-  uint16_t first[kMaxExperts + 1];          // first row of each chosen expert in h; rows of all behind the last
+  uint16_t slot[kMaxExperts];               // place of each chosen expert
+  uint16_t expert[kMaxExperts];             // chosen experts, ascending
+  uint16_t first[kMaxExperts + 1];          // first row of each in h; behind the last, the rows of all
+  uint8_t token[kSliceTokens * kMaxTopK];   // token of each row
+  float weight[kSliceTokens * kMaxTopK];    // weight of each row
   int chosen;
 };
-// All threads; pairs whose weight is 0 are left out.
+// All threads of the block.
 __device__ __forceinline__ void build_lists(Lists& l, const ExpertsArgs& a) {
+  const int pairs = a.T * a.top_k;
+  if (pairs <= 32) {
+    // a pair per lane of the first warp: the same experts find one another without a table
+    const int lane = threadIdx.x & 31;
+    if (threadIdx.x < 32) {
+      const float w = lane < pairs ? a.weights[lane] : 0.0f;
+      const int e = lane < pairs && w != 0.0f ? a.ids[lane] : kMaxExperts + lane;
+      const unsigned same = __match_any_sync(0xffffffffu, e), below = (1u << lane) - 1;
+      const bool on = e < kMaxExperts, leads = on && (same & below) == 0;
+      // places by expert: how many leaders have smaller ones, and how many pairs
+      int slot = 0, first = 0;
+      const unsigned leaders = __ballot_sync(0xffffffffu, leads);
+      for (int i = 0; i < pairs; ++i) {
+        const int o = __shfl_sync(0xffffffffu, e, i);
+        if (o < e) slot += leaders >> i & 1, ++first;
+      }
+      if (on) {
+        const int row = first + __popc(same & below);
+        l.token[row] = (uint8_t)(lane / a.top_k);
+        l.weight[row] = w;
+      }
+      if (leads) l.expert[slot] = (uint16_t)e, l.first[slot] = (uint16_t)first;
+      const int rows = __popc(__ballot_sync(0xffffffffu, on));
+      if (lane == 0) l.chosen = __popc(leaders), l.first[__popc(leaders)] = (uint16_t)rows;
+    }
+    __syncthreads();
+    return;
+  }
   for (int e = threadIdx.x; e < a.E; e += blockDim.x) l.tokens[e] = 0;
   __syncthreads();
-  for (int p = threadIdx.x; p < a.T * a.top_k; p += blockDim.x)
-    if (__ldg(a.weights + p) != 0.0f) atomicOr(&l.tokens[__ldg(a.ids + p)], 1ull << (p / a.top_k));
+  for (int p = threadIdx.x; p < pairs; p += blockDim.x)
+    if (a.weights[p] != 0.0f) atomicOr(&l.tokens[a.ids[p]], 1ull << (p / a.top_k));
   __syncthreads();
   if (threadIdx.x < 32) {
     const int lane = threadIdx.x;
@@ -155,6 +202,7 @@ __device__ __forceinline__ void build_lists(Lists& l, const ExpertsArgs& a) {
       }
       if (n != 0) {
         const int slot = slots + __popc(some & ((1u << lane) - 1));
+        l.slot[base + lane] = (uint16_t)slot;
         l.expert[slot] = (uint16_t)(base + lane);
         l.first[slot] = (uint16_t)(rows + upto - n);
       }
@@ -164,78 +212,126 @@ __device__ __forceinline__ void build_lists(Lists& l, const ExpertsArgs& a) {
     if (lane == 0) l.chosen = slots, l.first[slots] = (uint16_t)rows;
   }
   __syncthreads();
-}
-// The n-th token of a set (n below its size).
-__device__ __forceinline__ int nth_token(unsigned long long set, int n) {
-  const uint32_t lo = (uint32_t)set, hi = (uint32_t)(set >> 32);
-  const int c = __popc(lo);
-  return n < c ? __fns(lo, 0, n + 1) : 32 + __fns(hi, 0, n - c + 1);
+  for (int p = threadIdx.x; p < pairs; p += blockDim.x) {
+    const float w = a.weights[p];
+    if (w == 0.0f) continue;
+    const int e = a.ids[p], t = p / a.top_k;
+    const int row = l.first[l.slot[e]] + __popcll(l.tokens[e] & ((1ull << t) - 1));
+    l.token[row] = (uint8_t)t;
+    l.weight[row] = w;
+  }
+  __syncthreads();
 }
 
 // ---- gate and up --------------------------------------------------------------------------
-template <int DT, int NT, bool SMALL>
+#ifndef UPRING
+#define UPRING 3
+#endif
+#ifndef DOWNRING
+#define DOWNRING 6
+#endif
+constexpr int kUpDepth = UPRING, kDownDepth = DOWNRING;
+
+// An item is an expert, 8 / split row tiles, and 8 NT of the expert's tokens; a block takes every
+// gridDim.x-th, and has the next one's first tiles on the way while it finishes one.
+template <int DT, int NT, bool SMALL, bool ZEROS>
 __global__ void __launch_bounds__(kExpertWarps * 32)
-k_experts_up(const __grid_constant__ ExpertsArgs a) {
+k_experts_up(const __grid_constant__ ExpertsArgs a, int split) {
+  using In = Input<DT>;
+  using Tiles = Ring<2, 1, SMALL, ZEROS>;
+  constexpr int P = In::kParts == 3 ? 3 : 2;
   __shared__ Lists lists;
-  __shared__ float part[kExpertWarps][2][NT * 8][17];
-  __shared__ float weight[kSliceTokens];
-  constexpr int P = Input<DT>::kParts == 3 ? 3 : 2;
+  extern __shared__ __align__(128) uint8_t smem[];
+  float* sums = reinterpret_cast<float*>(smem + kExpertWarps * kUpDepth * Tiles::kSlot);   // [warp][token][33]
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
   griddep_launch();
   griddep_wait();
   build_lists(lists, a);
-  if ((int)blockIdx.y >= lists.chosen) return;
-  const int slot = blockIdx.y, expert = lists.expert[slot];
-  const unsigned long long tokens = lists.tokens[expert];
-  const int count = __popcll(tokens);
-  for (int p = threadIdx.x; p < a.T * a.top_k; p += blockDim.x)
-    if (__ldg(a.ids + p) == expert) weight[p / a.top_k] = __ldg(a.weights + p);
-  const Packed gate = expert_of(a.gate, expert, a.gate_units, a.gate_scales);
-  const Packed up = expert_of(a.up, expert, a.gate_units, a.gate_scales);
-  const long tile_K = blockIdx.x;
-  const long at = tile_K * gate.tiles_C * 64 + lane;
-  for (int n0 = 0; n0 < count; n0 += NT * 8) {
-    float acc_g[NT][4], acc_u[NT][4];
+  const int tiles_K = (a.I + 15) / 16, per_block = kExpertWarps / split, blocks_K = (tiles_K + per_block - 1) / per_block;
+  const int part = warp % split;
+  const int c0 = (int)((long)a.gate.tiles_C * part / split), c1 = (int)((long)a.gate.tiles_C * (part + 1) / split);
+  const uint32_t ring = smem_u32(smem) + warp * kUpDepth * Tiles::kSlot, ring_end = ring + kUpDepth * Tiles::kSlot;
+  const int whole = a.vec ? min(c1, a.D >> 7) : c0;         // tiles inside the rows of x, and aligned
+  int slot = blockIdx.x / blocks_K, block_K = blockIdx.x - slot * blocks_K, n0 = 0;
+  Tiles tiles;
+  auto begin = [&]() {
+    if (slot < lists.chosen) {
+      const int tile_K = min(block_K * per_block + warp / split, tiles_K - 1), expert = lists.expert[slot];
+      const Stream from[2] = {stream_of(expert_of(a.gate, expert, a.gate_units, a.gate_scales), tile_K),
+                              stream_of(expert_of(a.up, expert, a.gate_units, a.gate_scales), tile_K)};
+      tiles.start(from, a.gate, c0, c1, lane);
+    }
+#pragma unroll
+    for (int d = 0; d < kUpDepth; ++d) {
+      if (slot < lists.chosen && c0 + d < c1) tiles.fill(ring + d * Tiles::kSlot, lane);
+      Tiles::commit();
+    }
+  };
+  begin();
+  while (slot < lists.chosen) {
+    const int first = lists.first[slot], count = lists.first[slot + 1] - first;
+    float acc[2][NT][4];
     const char* row[NT];
+    const char* next[NT];
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
-      acc_g[n][0] = acc_g[n][1] = acc_g[n][2] = acc_g[n][3] = 0.0f;
-      acc_u[n][0] = acc_u[n][1] = acc_u[n][2] = acc_u[n][3] = 0.0f;
-      row[n] = a.x + nth_token(tokens, min(n0 + 8 * n + g, count - 1)) * a.x_row;
+      acc[0][n][0] = acc[0][n][1] = acc[0][n][2] = acc[0][n][3] = 0.0f;
+      acc[1][n][0] = acc[1][n][1] = acc[1][n][2] = acc[1][n][3] = 0.0f;
+      row[n] = a.x + lists.token[first + min(n0 + 8 * n + g, count - 1)] * a.x_row;
+      next[n] = row[n] + (c0 * 128l + 8 * t) * In::kBytes;
     }
-    for (int c = warp; c < gate.tiles_C; c += kExpertWarps) {
-      const uint4 g0 = __ldg(gate.codes + at + c * 64l), g1 = __ldg(gate.codes + at + c * 64l + 32);
-      const uint4 u0 = __ldg(up.codes + at + c * 64l), u1 = __ldg(up.codes + at + c * 64l + 32);
-      Input<DT> x[NT][4];
+    uint32_t at = ring;
+    for (int c = c0; c < c1; ++c) {
+      In x[NT][4];
+      if (c < whole) {
+        load_tile<DT, NT>(x, next);
+      } else {
 #pragma unroll
-      for (int n = 0; n < NT; ++n)
+        for (int n = 0; n < NT; ++n)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) x[n][i] = load_input<DT>(row[n], c * 128 + 32 * i + 8 * t, a.D, a.vec, 0);
-      tile_mma<SMALL, NT>(acc_g, gate, tile_K, c, g0, g1, x, 0, g);
-      tile_mma<SMALL, NT>(acc_u, up, tile_K, c, u0, u1, x, 0, g);
+          for (int i = 0; i < 4; ++i) x[n][i] = load_input<DT>(row[n], c * 128 + 32 * i + 8 * t, a.D, a.vec, 0);
+      }
+#pragma unroll
+      for (int n = 0; n < NT; ++n) next[n] += 128 * In::kBytes;
+      Tiles::template wait<kUpDepth - 1>();
+      tile_mma<SMALL, ZEROS, Tiles, NT>(acc[0], at, 0, a.gate, x, 0, lane);
+      tile_mma<SMALL, ZEROS, Tiles, NT>(acc[1], at, 1, a.up, x, 0, lane);
+      __syncwarp();            // the slot has been read
+      if (c + kUpDepth < c1) tiles.fill(at, lane);
+      Tiles::commit();
+      at = at + Tiles::kSlot == ring_end ? ring : at + Tiles::kSlot;
     }
-    __syncthreads();   // the sums of the tokens in front have been read, and `weight` is complete
+    const int this_K = block_K * per_block, this_n0 = n0;
+    if ((n0 += NT * 8) >= count) {
+      n0 = 0;
+      const int item = slot * blocks_K + block_K + gridDim.x;
+      slot = item / blocks_K; block_K = item - slot * blocks_K;
+    }
+    __syncthreads();           // the sums in front have been read
 #pragma unroll
     for (int n = 0; n < NT; ++n)
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        part[warp][0][8 * n + 2 * t + (e & 1)][g + 8 * (e >> 1)] = acc_g[n][e];
-        part[warp][1][8 * n + 2 * t + (e & 1)][g + 8 * (e >> 1)] = acc_u[n][e];
+        float* s = sums + (warp * NT * 8 + 8 * n + 2 * t + (e & 1)) * 33 + g + 8 * (e >> 1);
+        s[0] = acc[0][n][e];
+        s[16] = acc[1][n][e];
       }
+    begin();
     __syncthreads();
-    for (int e = threadIdx.x; e < NT * 8 * 16; e += kExpertWarps * 32) {
-      const int n = n0 + (e >> 4);
-      const int i = (int)tile_K * 16 + (e & 15);
-      if (n >= count || i >= a.I) continue;
+    for (int e = threadIdx.x; e < per_block * NT * 8 * 16; e += kExpertWarps * 32) {
+      const int k = e & 15, m = (e >> 4) % (NT * 8), v = (e >> 4) / (NT * 8);
+      const int i = (this_K + v) * 16 + k;
+      if (this_n0 + m >= count || i >= a.I) continue;
       float gs = 0.0f, us = 0.0f;
-#pragma unroll
-      for (int v = 0; v < kExpertWarps; ++v) {
-        gs = __fadd_rn(gs, part[v][0][e >> 4][e & 15]);
-        us = __fadd_rn(us, part[v][1][e >> 4][e & 15]);
+      for (int w = 0; w < split; ++w) {
+        const float* s = sums + ((v * split + w) * NT * 8 + m) * 33 + k;
+        gs = __fadd_rn(gs, s[0]);
+        us = __fadd_rn(us, s[16]);
       }
       const float silu = __fdiv_rn(gs, __fadd_rn(1.0f, expf(-gs)));
-      float h = keep_nan(__fmul_rn(__fmul_rn(silu, us), weight[nth_token(tokens, n)]));
-      uint16_t* to = a.h + (lists.first[slot] + n) * a.h_row + i;
+      const int row_h = first + this_n0 + m;
+      float h = keep_nan(__fmul_rn(__fmul_rn(silu, us), lists.weight[row_h]));
+      uint16_t* to = a.h + row_h * a.h_row + i;
 #pragma unroll
       for (int p = 0; p < P; ++p) {
         to[p * a.h_plane] = (uint16_t)(__float_as_uint(h) >> 16);
@@ -246,11 +342,13 @@ k_experts_up(const __grid_constant__ ExpertsArgs a) {
 }
 
 // ---- down -----------------------------------------------------------------------------------
-template <int P, int NT, bool SMALL>
+template <int P, int NT, bool SMALL, bool ZEROS>
 __global__ void __launch_bounds__(kExpertWarps * 32)
-k_experts_down(const __grid_constant__ ExpertsArgs a) {
+k_experts_down(const __grid_constant__ ExpertsArgs a, int split) {
+  using Tiles = Ring<1, 1, SMALL, ZEROS>;
   __shared__ Lists lists;
-  extern __shared__ float sums[];    // [warp][T][17], then [T][17]
+  extern __shared__ __align__(128) uint8_t smem[];
+  float* sums = reinterpret_cast<float*>(smem + kExpertWarps * kDownDepth * Tiles::kSlot);   // [warp][T][17], then [T][17]
   const cg::cluster_group cluster = cg::this_cluster();
   const int S = (int)cluster.num_blocks(), rank = (int)cluster.block_rank();
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
@@ -259,87 +357,197 @@ k_experts_down(const __grid_constant__ ExpertsArgs a) {
   griddep_wait();
   build_lists(lists, a);
   float* mine = sums + warp * a.T * 17;
-  const long tile_K = blockIdx.x / S;
-  const int tiles = a.down.tiles_C;
-  for (int u = rank * kExpertWarps + warp; u < lists.chosen * tiles; u += kExpertWarps * S) {
-    const int slot = u / tiles, c = u - slot * tiles, expert = lists.expert[slot];
-    const unsigned long long tokens = lists.tokens[expert];
-    const int count = __popcll(tokens);
-    const Packed w = expert_of(a.down, expert, a.down_units, a.down_scales);
-    const uint4* codes = w.codes + (tile_K * tiles + c) * 64l + lane;
-    const uint4 u0 = __ldg(codes), u1 = __ldg(codes + 32);
-    for (int n0 = 0; n0 < count; n0 += NT * 8) {
-      float acc[NT][4];
-      Planes<P> x[NT][4];
-#pragma unroll
-      for (int n = 0; n < NT; ++n) {
-        acc[n][0] = acc[n][1] = acc[n][2] = acc[n][3] = 0.0f;
-        const uint16_t* row = a.h + (lists.first[slot] + min(n0 + 8 * n + g, count - 1)) * a.h_row;
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-#pragma unroll
-          for (int p = 0; p < P; ++p)
-            x[n][i].v[p] = load_input<WINO_BF16>(reinterpret_cast<const char*>(row + p * a.h_plane),
-                                                 c * 128 + 32 * i + 8 * t, a.I, true, 0).v;
-      }
-      tile_mma<SMALL, NT>(acc, w, tile_K, c, u0, u1, x, 0, g);
-#pragma unroll
-      for (int n = 0; n < NT; ++n)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const int at = n0 + 8 * n + 2 * t + (e & 1);
-          if (at < count) {
-            float* s = mine + nth_token(tokens, at) * 17 + g + 8 * (e >> 1);
-            *s = __fadd_rn(*s, acc[n][e]);
-          }
-        }
+  const int per_block = kExpertWarps / split, tiles_K = (a.D + 15) / 16, tiles = a.down.tiles_C;
+  const int tile_K = (int)(blockIdx.x / S) * per_block + warp / split;
+  // this warp's part of the tiles of all chosen experts, [expert][tile of inputs]
+  const int part = rank * split + warp % split, shared_by = split * S;
+  const int all = lists.chosen * tiles;
+  const int u0 = (int)((long)all * part / shared_by), u1 = tile_K < tiles_K ? (int)((long)all * (part + 1) / shared_by) : u0;
+  const uint32_t ring = smem_u32(smem) + warp * kDownDepth * Tiles::kSlot, ring_end = ring + kDownDepth * Tiles::kSlot;
+  int slot = 0, c = 0, fill_slot = 0, fill_c = 0;
+  Tiles from;
+  auto start = [&](int s, int at) {
+    const Stream w[1] = {stream_of(expert_of(a.down, lists.expert[s], a.down_units, a.down_scales), tile_K)};
+    from.start(w, a.down, at, tiles, lane);
+  };
+  if (u0 < u1) {
+    slot = fill_slot = u0 / tiles;
+    c = fill_c = u0 - slot * tiles;
+    start(slot, c);
+  }
+  auto fill = [&](uint32_t to) {
+    from.fill(to, lane);
+    if (++fill_c == tiles) {
+      fill_c = 0;
+      if (++fill_slot < lists.chosen) start(fill_slot, 0);
     }
-    __syncwarp();
+  };
+#pragma unroll
+  for (int d = 0; d < kDownDepth; ++d) {
+    if (u0 + d < u1) fill(ring + d * Tiles::kSlot);
+    Tiles::commit();
+  }
+  float acc[NT][4];
+#pragma unroll
+  for (int n = 0; n < NT; ++n) acc[n][0] = acc[n][1] = acc[n][2] = acc[n][3] = 0.0f;
+  uint32_t at = ring;
+  const int whole = a.I >> 7;                       // tiles inside the rows of h
+  int first = 0, count = 0;
+  const uint16_t* row[NT];                          // of h, of the first tokens
+  auto row_of = [&](int n) { return a.h + (first + min(n + g, count - 1)) * a.h_row + 8 * t; };
+  auto enter = [&]() {
+    first = lists.first[slot]; count = lists.first[slot + 1] - first;
+#pragma unroll
+    for (int n = 0; n < NT; ++n) row[n] = row_of(8 * n);
+  };
+  auto load = [&](Planes<P> (&x)[4], const uint16_t* from_h) {
+    if (c < whole) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int p = 0; p < P; ++p) x[i].v[p] = *reinterpret_cast<const uint4*>(from_h + p * a.h_plane + c * 128 + 32 * i);
+    } else {
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int p = 0; p < P; ++p)
+          x[i].v[p] = load_input<WINO_BF16>(reinterpret_cast<const char*>(from_h + p * a.h_plane - 8 * t),
+                                            c * 128 + 32 * i + 8 * t, a.I, true, 0).v;
+    }
+  };
+  if (u0 < u1) enter();
+  for (int u = u0; u < u1; ++u) {
+    Planes<P> x[NT][4];
+#pragma unroll
+    for (int n = 0; n < NT; ++n) load(x[n], row[n]);
+    Tiles::template wait<kDownDepth - 1>();
+    tile_mma<SMALL, ZEROS, Tiles, NT>(acc, at, 0, a.down, x, 0, lane);
+    const bool last = c + 1 == tiles || u + 1 == u1, more = count > NT * 8;
+    // tokens of the expert, 8 NT at a time; up to that many, sums stay in registers over its tiles
+    if (last || more) {
+      for (int n0 = 0;;) {
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const int m = n0 + 8 * n + 2 * t + (e & 1);
+            if (m < count) {
+              float* s = mine + lists.token[first + m] * 17 + g + 8 * (e >> 1);
+              *s = __fadd_rn(*s, acc[n][e]);
+            }
+            acc[n][e] = 0.0f;
+          }
+        if ((n0 += NT * 8) >= count) break;
+#pragma unroll
+        for (int n = 0; n < NT; ++n) load(x[n], row_of(n0 + 8 * n));
+        tile_mma<SMALL, ZEROS, Tiles, NT>(acc, at, 0, a.down, x, 0, lane);
+      }
+    }
+    __syncwarp();              // the slot has been read, and `mine` is everyone's
+    if (u + kDownDepth < u1) fill(at);
+    Tiles::commit();
+    if (++c == tiles) {
+      c = 0;
+      ++slot;
+      if (u + 1 < u1) enter();
+    }
+    at = at + Tiles::kSlot == ring_end ? ring : at + Tiles::kSlot;
   }
   __syncthreads();
-  float* total = sums + kExpertWarps * a.T * 17;
-  for (int e = threadIdx.x; e < a.T * 16; e += blockDim.x) {
+  // outputs of the block: [row tile][token][16], summed over the warps that share the row tile; a cluster's
+  // blocks leave their sums where their first warp's were
+  const int outputs = per_block * a.T * 16;
+  auto finish = [&](int v, int m, int k, float s) {
+    const long out = ((long)(blockIdx.x / S) * per_block + v) * 16 + k;
+    if (out < a.D) store_output(a.out, m * a.y_row + out, s, 0.0f);
+  };
+  for (int e = threadIdx.x; e < outputs; e += kExpertWarps * 32) {
+    const int k = e & 15, m = (e >> 4) % a.T, v = (e >> 4) / a.T;
     float s = 0.0f;
-#pragma unroll
-    for (int v = 0; v < kExpertWarps; ++v) s = __fadd_rn(s, sums[(v * a.T + (e >> 4)) * 17 + (e & 15)]);
-    total[(e >> 4) * 17 + (e & 15)] = s;
+    for (int i = 0; i < split; ++i) s = __fadd_rn(s, sums[((v * split + i) * a.T + m) * 17 + k]);
+    if (S > 1) sums[(v * split * a.T + m) * 17 + k] = s;
+    else finish(v, m, k, s);
   }
-  if (S > 1) cluster.sync();
-  else __syncthreads();
-  for (int e = threadIdx.x * S + rank; e < a.T * 16; e += blockDim.x * S) {
-    const int m = e >> 4;
-    const long k = tile_K * 16 + (e & 15);
+  if (S == 1) return;
+  cluster.sync();
+  for (int e = threadIdx.x * S + rank; e < outputs; e += kExpertWarps * 32 * S) {
+    const int k = e & 15, m = (e >> 4) % a.T, v = (e >> 4) / a.T;
     float s = 0.0f;
-    for (int b = 0; b < S; ++b)
-      s = __fadd_rn(s, (S > 1 ? cluster.map_shared_rank(total, b) : total)[m * 17 + (e & 15)]);
-    if (k < a.D) store_output(a.out, m * a.y_row + k, s, 0.0f);
+    for (int b = 0; b < S; ++b) s = __fadd_rn(s, cluster.map_shared_rank(sums, b)[(v * split * a.T + m) * 17 + k]);
+    finish(v, m, k, s);
   }
-  if (S > 1) cluster.sync();   // no block leaves while another reads its sums
+  cluster.sync();   // no block leaves while another reads its sums
 }
 
 namespace {
 
+#ifndef UPBLOCKS
+#define UPBLOCKS 2
+#endif
+#ifndef DOWNBLOCKS
+#define DOWNBLOCKS 2
+#endif
+// Warps that share one row tile's inputs: a power of two up to `most`, no more warps than there are, and
+// no more than tiles.
+int shared_by(long row_tiles, long tiles, int most, long warps) {
+  int n = 1;
+  while (n < most && row_tiles * n * 2 <= warps && n * 2 <= tiles) n *= 2;
+  return n;
+}
+
+template <int DT, int NT, bool SMALL, bool ZEROS>
+int launch_up(const ExpertsArgs& a, long slots, int num_sms, int dev, cudaStream_t st) {
+  constexpr size_t smem = (size_t)kExpertWarps * (kUpDepth * Ring<2, 1, SMALL, ZEROS>::kSlot + NT * 8 * 33 * sizeof(float));
+  const long tiles_K = (a.I + 15) / 16;
+  const int split = shared_by(tiles_K * slots, a.gate.tiles_C, kExpertWarps, (long)UPBLOCKS * kExpertWarps * num_sms);
+  const long items = (tiles_K + kExpertWarps / split - 1) / (kExpertWarps / split) * slots;
+  const long most = (long)UPBLOCKS * num_sms;
+  static DeviceOnce once;
+  auto kernel = k_experts_up<DT, NT, SMALL, ZEROS>;
+  const int rc = set_max_smem(once, dev, kernel, smem);
+  if (rc != 0) return rc;
+  return launch_kernel(kernel, dim3((unsigned)(items < most ? items : most)), dim3(kExpertWarps * 32), smem, st, true, a, split);
+}
+
+template <int P, int NT, bool SMALL, bool ZEROS>
+int launch_down(const ExpertsArgs& a, long slots, int num_sms, int dev, cudaStream_t st) {
+  constexpr size_t ring = (size_t)kExpertWarps * kDownDepth * Ring<1, 1, SMALL, ZEROS>::kSlot;
+  const size_t smem = ring + (size_t)kExpertWarps * a.T * 17 * sizeof(float);
+  const long tiles_K = (a.D + 15) / 16;
+  const int by = shared_by(tiles_K, (a.I + 127l) / 128 * slots, 8 * kExpertWarps, (long)DOWNBLOCKS * kExpertWarps * num_sms);
+  const int split = by < kExpertWarps ? by : kExpertWarps, S = by / split;
+  const long blocks = (tiles_K + kExpertWarps / split - 1) / (kExpertWarps / split);
+  static DeviceOnce once;
+  auto kernel = k_experts_down<P, NT, SMALL, ZEROS>;
+  const int rc = set_max_smem(once, dev, kernel, ring + (size_t)kExpertWarps * kSliceTokens * 17 * sizeof(float));
+  if (rc != 0) return rc;
+  return launch_kernel_cluster(kernel, dim3((unsigned)(blocks * S)), dim3(kExpertWarps * 32), (unsigned)S, smem, st,
+                               true, a, split);
+}
+
 template <int DT, int NT>
 int launch_slice(const ExpertsArgs& a, int num_sms, cudaStream_t st) {
   constexpr int P = Input<DT>::kParts == 3 ? 3 : 2;
-  int rc = launch_kernel(k_experts_route<DT>, dim3((unsigned)a.T), dim3(kRouteThreads), 0, st, true, a);
+  int dev = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess) return WINO_ERR_CUDA;
+  // blocks that share a token's experts, eight or more each, while there are SMs for them
+  int S = 1;
+  while (S < 8 && (long)a.T * S * 2 <= num_sms && S * 2 * (kRouteThreads / 32) <= a.E) S *= 2;
+  int rc = launch_kernel_cluster(k_experts_route<DT>, dim3((unsigned)(a.T * S)), dim3(kRouteThreads), (unsigned)S, 0, st, true, a);
   if (rc != 0) return rc;
   const long slots = (long)a.T * a.top_k < a.E ? (long)a.T * a.top_k : a.E;
-  auto up = a.gate.group < 128 ? k_experts_up<DT, NT, true> : k_experts_up<DT, NT, false>;
-  rc = launch_kernel(up, dim3((unsigned)((a.I + 15) / 16), (unsigned)slots), dim3(kExpertWarps * 32), 0, st, true, a);
-  if (rc != 0) return rc;
-  auto down = a.down.group < 128 ? k_experts_down<P, NT, true> : k_experts_down<P, NT, false>;
-  const size_t smem = (size_t)(kExpertWarps + 1) * a.T * 17 * sizeof(float);   // at most 38.25 KB
-  const long tiles_K = (a.D + 15) / 16, units = (a.I + 127) / 128 * slots;
-  int S = 1;
-  while (S < 8 && tiles_K * S < 2l * num_sms && (long)S * kExpertWarps < units) S *= 2;
-  return launch_kernel_cluster(down, dim3((unsigned)(tiles_K * S)), dim3(kExpertWarps * 32), (unsigned)S, smem, st,
-                               true, a);
+  auto up = a.gate.group < 128 ? (a.gate.zeros ? launch_up<DT, NT, true, true> : launch_up<DT, NT, true, false>)
+                               : (a.gate.zeros ? launch_up<DT, NT, false, true> : launch_up<DT, NT, false, false>);
+  if ((rc = up(a, slots, num_sms, dev, st)) != 0) return rc;
+  auto down = a.down.group < 128 ? (a.down.zeros ? launch_down<P, NT, true, true> : launch_down<P, NT, true, false>)
+                                 : (a.down.zeros ? launch_down<P, NT, false, true> : launch_down<P, NT, false, false>);
+  return down(a, slots, num_sms, dev, st);
 }
 
 template <int DT>
 int launch_type(const ExpertsArgs& a, int num_sms, cudaStream_t st) {
-  return a.T <= 8 ? launch_slice<DT, 1>(a, num_sms, st) : launch_slice<DT, 2>(a, num_sms, st);
+  // 16 of an expert's tokens at a time where it has more than 6 on average
+  return (long)a.T * a.top_k <= 6l * a.E || a.T <= 8 ? launch_slice<DT, 1>(a, num_sms, st) : launch_slice<DT, 2>(a, num_sms, st);
 }
 
 long h_row_of(int I) { return (I + 7l) / 8 * 8; }

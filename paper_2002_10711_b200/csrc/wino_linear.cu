@@ -1,9 +1,10 @@
 // y = x W^T + bias with 4-bit weights and group scales, for few rows of x: warp MMAs on unpacked codes.
 //
-// Bound by reading the codes: 16 outputs x 128 inputs are 1 KB, read once.  A block owns 16 outputs and
-// up to 8 NT rows of x; its eight warps take the 1 KB tiles of its outputs in turn, and where there are
-// too few blocks to fill the GPU, the S blocks of a cluster share the tiles.  Sums of warps meet in
-// shared memory, those of blocks through the cluster's, in a fixed order: no workspace, no atomics.
+// Bound by reading the codes: 16 outputs x 128 inputs are 1 KB, read once.  A warp streams the tiles of R row
+// tiles (16 R outputs) over a part of the inputs through a ring of asynchronous copies, against up to 8 NT
+// rows of x, which it reads from the L1 cache in the form of MMA operands.  `split` warps of a block, and the
+// S blocks of a cluster where there are too few outputs to fill the GPU, share the inputs; their sums
+// meet in shared memory in a fixed order: no workspace, no atomics.
 #include <cooperative_groups.h>
 
 #include "wino_packed.cuh"
@@ -20,95 +21,172 @@ struct LinearArgs {
   long y_row;       // elements
   const float* bias;
   int M, z_x, vec;
+  int split;        // warps of a block that share a row tile's inputs
 };
 
 constexpr int kRowsWarps = 8;
+#ifndef RING
+#define RING 3
+#endif
 
-template <int DT, int NT, bool SMALL>
+template <int DT, int NT, int R, bool SMALL, bool ZEROS>
 __global__ void __launch_bounds__(kRowsWarps * 32)
 k_linear_rows(const __grid_constant__ LinearArgs a) {
-  __shared__ float part[kRowsWarps][NT * 8][17];   // [warp][row of x][output], one bank apart
-  __shared__ float total[NT * 8][17];
+  using In = Input<DT>;
+  constexpr int T = 2 / R;                           // tiles of inputs a slot
+  using Tiles = Ring<R, T, SMALL, ZEROS>;
+  constexpr int kDepth = RING;
+  constexpr int kSums = R * 16 + 1;                  // floats of a row of sums: one bank apart
+  extern __shared__ __align__(128) uint8_t smem[];
   const cg::cluster_group cluster = cg::this_cluster();
   const int S = (int)cluster.num_blocks(), rank = (int)cluster.block_rank();
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
-  const long tile_K = blockIdx.x / S;
+  const int tiles_K = (a.w.K + 15) / 16;
+  const int shared_by = a.split * S, part = rank * a.split + warp % a.split;
+  const int unit = (int)(blockIdx.x / S) * (kRowsWarps / a.split) + warp / a.split;    // R row tiles
   const int m0 = blockIdx.y * NT * 8;
+  const int c0 = (int)((long)a.w.tiles_C * part / shared_by), c1 = (int)((long)a.w.tiles_C * (part + 1) / shared_by);
   griddep_launch();
   griddep_wait();
 
-  float acc[NT][4];
+  float acc[R][NT][4];
 #pragma unroll
-  for (int n = 0; n < NT; ++n) acc[n][0] = acc[n][1] = acc[n][2] = acc[n][3] = 0.0f;
-  const char* row[NT];
+  for (int r = 0; r < R; ++r)
 #pragma unroll
-  for (int n = 0; n < NT; ++n) row[n] = a.x + min(m0 + 8 * n + g, a.M - 1) * a.x_row;
-  const uint4* codes = a.w.codes + tile_K * a.w.tiles_C * 64 + lane;
-  const int step = kRowsWarps * S;
-  int c = rank * kRowsWarps + warp;
-  uint4 u0, u1;
-  Input<DT> x[NT][4];
-  auto fetch = [&](int tile) {
-    u0 = __ldg(codes + tile * 64l);
-    u1 = __ldg(codes + tile * 64l + 32);
+    for (int n = 0; n < NT; ++n) acc[r][n][0] = acc[r][n][1] = acc[r][n][2] = acc[r][n][3] = 0.0f;
+  if (unit * R < tiles_K) {
+    Stream w[R];
+#pragma unroll
+    for (int r = 0; r < R; ++r) w[r] = stream_of(a.w, min(unit * R + r, tiles_K - 1));
+    const char* row[NT];
+    const char* next[NT];
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+      row[n] = a.x + min(m0 + 8 * n + g, a.M - 1) * a.x_row;
+      next[n] = row[n] + (c0 * 128l + 8 * t) * In::kBytes;
+    }
+    const uint32_t ring = smem_u32(smem) + warp * kDepth * Tiles::kSlot, ring_end = ring + kDepth * Tiles::kSlot;
+    Tiles tiles;
+    tiles.start(w, a.w, c0, c1, lane);
+#pragma unroll
+    for (int d = 0; d < kDepth; ++d) {
+      if (c0 + d * T < c1) tiles.fill(ring + d * Tiles::kSlot, lane);
+      Tiles::commit();
+    }
+    const int whole = a.vec ? min(c1, a.w.C >> 7) : c0;     // tiles inside the rows of x, and aligned
+    uint32_t slot = ring;
+    for (int c = c0; c < c1; c += T) {
+#pragma unroll
+      for (int j = 0; j < T; ++j) {
+        if (j > 0 && c + j >= c1) break;
+        In x[NT][4];
+        if (c + j < whole) {
+          load_tile<DT, NT>(x, next);
+        } else {
+#pragma unroll
+          for (int n = 0; n < NT; ++n)
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+              x[n][i] = load_input<DT>(row[n], (c + j) * 128 + 32 * i + 8 * t, a.w.C, a.vec, a.z_x);
+        }
+#pragma unroll
+        for (int n = 0; n < NT; ++n) next[n] += 128 * In::kBytes;
+        if (j == 0) Tiles::template wait<kDepth - 1>();
+#pragma unroll
+        for (int r = 0; r < R; ++r) tile_mma<SMALL, ZEROS, Tiles, NT>(acc[r], slot, r * T + j, a.w, x, a.z_x, lane);
+      }
+      __syncwarp();          // the slot has been read
+      if (tiles.c < c1) tiles.fill(slot, lane);
+      Tiles::commit();
+      slot = slot + Tiles::kSlot == ring_end ? ring : slot + Tiles::kSlot;
+    }
+  }
+  __syncthreads();           // the rings are read: their place is that of the sums
+  float* sums = reinterpret_cast<float*>(smem);           // [warp][row of x][output]
+  float* total = sums + kRowsWarps * NT * 8 * kSums;
+#pragma unroll
+  for (int r = 0; r < R; ++r)
 #pragma unroll
     for (int n = 0; n < NT; ++n)
 #pragma unroll
-      for (int i = 0; i < 4; ++i)
-        x[n][i] = load_input<DT>(row[n], tile * 128 + 32 * i + 8 * t, a.w.C, a.vec, a.z_x);
-  };
-  for (; c < a.w.tiles_C; c += step) {
-    fetch(c);
-    tile_mma<SMALL, NT>(acc, a.w, tile_K, c, u0, u1, x, a.z_x, g);
-  }
-#pragma unroll
-  for (int n = 0; n < NT; ++n) {
-    part[warp][8 * n + 2 * t][g] = acc[n][0];
-    part[warp][8 * n + 2 * t + 1][g] = acc[n][1];
-    part[warp][8 * n + 2 * t][g + 8] = acc[n][2];
-    part[warp][8 * n + 2 * t + 1][g + 8] = acc[n][3];
-  }
+      for (int e = 0; e < 4; ++e)
+        sums[(warp * NT * 8 + 8 * n + 2 * t + (e & 1)) * kSums + r * 16 + g + 8 * (e >> 1)] = acc[r][n][e];
   __syncthreads();
-  for (int e = threadIdx.x; e < NT * 8 * 16; e += kRowsWarps * 32) {
+  // outputs of the block: [unit][row of x][16 R]
+  const int outputs = kRowsWarps / a.split * NT * 8 * R * 16;
+  auto place = [&](int e, int& v, int& m, int& k) {
+    k = e % (R * 16);
+    m = e / (R * 16) % (NT * 8);
+    v = e / (R * 16 * NT * 8);
+  };
+  auto finish = [&](int v, int m, int k, float s) {
+    const long out = ((long)(blockIdx.x / S) * (kRowsWarps / a.split) + v) * R * 16 + k;
+    if (m0 + m < a.M && out < a.w.K) store_output(a.out, (m0 + m) * a.y_row + out, s, a.bias ? a.bias[out] : 0.0f);
+  };
+  for (int e = threadIdx.x; e < outputs; e += kRowsWarps * 32) {
+    int v, m, k;
+    place(e, v, m, k);
     float s = 0.0f;
-#pragma unroll
-    for (int v = 0; v < kRowsWarps; ++v) s = __fadd_rn(s, part[v][e >> 4][e & 15]);
-    total[e >> 4][e & 15] = s;
+    for (int i = 0; i < a.split; ++i) s = __fadd_rn(s, sums[((v * a.split + i) * NT * 8 + m) * kSums + k]);
+    if (S > 1) total[(v * NT * 8 + m) * kSums + k] = s;
+    else finish(v, m, k, s);
   }
-  if (S > 1) cluster.sync();
-  else __syncthreads();
+  if (S == 1) return;
+  cluster.sync();
   // block `rank` of the cluster finishes its share of the outputs
-  for (int e = threadIdx.x * S + rank; e < NT * 8 * 16; e += kRowsWarps * 32 * S) {
-    const int m = m0 + (e >> 4);
-    const long k = tile_K * 16 + (e & 15);
+  for (int e = threadIdx.x * S + rank; e < outputs; e += kRowsWarps * 32 * S) {
+    int v, m, k;
+    place(e, v, m, k);
     float s = 0.0f;
-    for (int b = 0; b < S; ++b)
-      s = __fadd_rn(s, S > 1 ? cluster.map_shared_rank(&total[0][0], b)[(e >> 4) * 17 + (e & 15)] : total[e >> 4][e & 15]);
-    if (m < a.M && k < a.w.K) store_output(a.out, m * a.y_row + k, s, a.bias ? __ldg(a.bias + k) : 0.0f);
+    for (int b = 0; b < S; ++b) s = __fadd_rn(s, cluster.map_shared_rank(total, b)[(v * NT * 8 + m) * kSums + k]);
+    finish(v, m, k, s);
   }
-  if (S > 1) cluster.sync();   // no block leaves while another reads its sums
+  cluster.sync();   // no block leaves while another reads its sums
 }
 
 namespace {
 
-template <int DT, int NT>
-int launch_rows(const LinearArgs& a, int num_sms, cudaStream_t st) {
-  const long tiles_K = (a.w.K + 15) / 16, slices = (a.M + NT * 8 - 1) / (NT * 8);
-  int S = 1;
-  while (S < 8 && tiles_K * slices * S < 2l * num_sms && S * kRowsWarps < a.w.tiles_C) S *= 2;
+#ifndef WARPS_PER_SM
+#define WARPS_PER_SM 16
+#endif
+template <int DT, int NT, int R, bool SMALL, bool ZEROS>
+int launch_rows(const LinearArgs& given, int num_sms, cudaStream_t st) {
+  LinearArgs a = given;
+  const long units = ((a.w.K + 15) / 16 + R - 1) / R, slices = (a.M + NT * 8 - 1) / (NT * 8);
   if (slices > 65535) return WINO_ERR_UNSUPPORTED;
-  const dim3 grid((unsigned)(tiles_K * S), (unsigned)slices);
-  auto kernel = a.w.group < 128 ? k_linear_rows<DT, NT, true> : k_linear_rows<DT, NT, false>;
-  return launch_kernel_cluster(kernel, grid, dim3(kRowsWarps * 32), (unsigned)S, 0, st, true, a);
+  // inputs shared by as many warps as it takes to have WARPS_PER_SM of them on every SM
+  int shared_by = 1;
+  while (shared_by < 64 && units * slices * shared_by < (long)WARPS_PER_SM * num_sms && shared_by * 2 <= a.w.tiles_C) shared_by *= 2;
+  a.split = shared_by < kRowsWarps ? shared_by : kRowsWarps;
+  const int S = shared_by / a.split;
+  const long blocks = (units + kRowsWarps / a.split - 1) / (kRowsWarps / a.split);
+  const dim3 grid((unsigned)(blocks * S), (unsigned)slices);
+  constexpr int kDepth = RING;
+  constexpr size_t ring = (size_t)kRowsWarps * kDepth * Ring<R, 2 / R, SMALL, ZEROS>::kSlot;
+  constexpr size_t sums = (size_t)2 * kRowsWarps * NT * 8 * (R * 16 + 1) * sizeof(float);
+  constexpr size_t smem = ring > sums ? ring : sums;
+  auto kernel = k_linear_rows<DT, NT, R, SMALL, ZEROS>;
+  static DeviceOnce once;
+  int dev = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess) return WINO_ERR_CUDA;
+  const int rc = set_max_smem(once, dev, kernel, smem);
+  if (rc != 0) return rc;
+  return launch_kernel_cluster(kernel, grid, dim3(kRowsWarps * 32), (unsigned)S, smem, st, true, a);
+}
+
+template <int DT, int NT, int R>
+int launch_groups(const LinearArgs& a, int num_sms, cudaStream_t st) {
+  if (a.w.zeros != nullptr)
+    return a.w.group < 128 ? launch_rows<DT, NT, R, true, true>(a, num_sms, st) : launch_rows<DT, NT, R, false, true>(a, num_sms, st);
+  return a.w.group < 128 ? launch_rows<DT, NT, R, true, false>(a, num_sms, st) : launch_rows<DT, NT, R, false, false>(a, num_sms, st);
 }
 
 template <int DT>
 int launch_type(const LinearArgs& a, int num_sms, cudaStream_t st) {
-  return a.M <= 8 ? launch_rows<DT, 1>(a, num_sms, st) : launch_rows<DT, 2>(a, num_sms, st);
+  return a.M <= 8 ? launch_groups<DT, 1, 1>(a, num_sms, st) : launch_groups<DT, 2, 2>(a, num_sms, st);
 }
 
 }  // namespace
-
 int launch_linear(const wino_linear_desc_t& d, const void* x, const float* bias, void* y, int num_sms,
                   cudaStream_t st) {
   LinearArgs a;

@@ -17,6 +17,7 @@
 
 #include "wino.h"
 #include "wino_launch.h"
+#include "wino_ptx.cuh"
 
 namespace wino {
 
@@ -95,6 +96,21 @@ __device__ __forceinline__ void mma_16816(float (&d)[4], uint32_t a0, uint32_t a
                  : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
 
+template <bool F16>
+__device__ __forceinline__ void mma_16816_from_0(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3,
+                                                 uint32_t b0, uint32_t b1) {
+  if (F16)
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, "
+        "{%10, %10, %10, %10};"
+        : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])
+        : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(0.0f));
+  else
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, "
+        "{%10, %10, %10, %10};"
+        : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])
+        : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(0.0f));
+}
+
 // Two floats -> a bf16 pair of their leading 8 significant bits (truncated: what is left is exact,
 // and nothing overflows), lower half first.
 __device__ __forceinline__ uint32_t truncate2(float lo, float hi) {
@@ -109,17 +125,18 @@ __device__ __forceinline__ float rest_of_any(float v) { return fabsf(v) <= 3.402
 // Top 16 bits that keep a NaN one whose payload is all in the lower bits.
 __device__ __forceinline__ float keep_nan(float v) { return v == v ? v : __uint_as_float(0x7FFF0000u); }
 
-// Eight consecutive inputs of one row of x, as loaded and as the B operand of two MMAs.
+// Eight consecutive inputs of one row of x, as loaded and as the B operand of two MMAs.  Loads are ordinary
+// ones (not of the read-only path): the kernel in front may have written x while this one was starting.
 //   PARTS  number of operands whose sum is x;  F16  their format
 template <int DT> struct Input;
 template <> struct Input<WINO_BF16> {
   static constexpr int kParts = 1, kBytes = 2;
   static constexpr bool kF16 = false;
   uint4 v;
-  __device__ __forceinline__ void load(const char* p) { v = __ldg(reinterpret_cast<const uint4*>(p)); }
+  __device__ __forceinline__ void load(const char* p) { v = *reinterpret_cast<const uint4*>(p); }
   __device__ __forceinline__ void clear(int) { v = make_uint4(0, 0, 0, 0); }
   __device__ __forceinline__ void set(int e, const char* p) {
-    const uint32_t h = __ldg(reinterpret_cast<const unsigned short*>(p));
+    const uint32_t h = *reinterpret_cast<const unsigned short*>(p);
     uint32_t& w = e < 2 ? v.x : e < 4 ? v.y : e < 6 ? v.z : v.w;
     w |= e & 1 ? h << 16 : h;
   }
@@ -135,14 +152,14 @@ template <> struct Input<WINO_FLOAT> {
   static constexpr bool kF16 = false;
   float v[8];
   __device__ __forceinline__ void load(const char* p) {
-    const float4 a = __ldg(reinterpret_cast<const float4*>(p)), b = __ldg(reinterpret_cast<const float4*>(p) + 1);
+    const float4 a = reinterpret_cast<const float4*>(p)[0], b = reinterpret_cast<const float4*>(p)[1];
     v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w; v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
   }
   __device__ __forceinline__ void clear(int) {
 #pragma unroll
     for (int e = 0; e < 8; ++e) v[e] = 0.0f;
   }
-  __device__ __forceinline__ void set(int e, const char* p) { v[e] = __ldg(reinterpret_cast<const float*>(p)); }
+  __device__ __forceinline__ void set(int e, const char* p) { v[e] = *reinterpret_cast<const float*>(p); }
   __device__ __forceinline__ void operand(int, uint32_t (&b)[kParts][4]) const {
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
@@ -158,12 +175,12 @@ template <> struct Input<WINO_INT8> {
   static constexpr int kParts = 1, kBytes = 1;
   static constexpr bool kF16 = true;
   uint2 v;
-  __device__ __forceinline__ void load(const char* p) { v = __ldg(reinterpret_cast<const uint2*>(p)); }
+  __device__ __forceinline__ void load(const char* p) { v = *reinterpret_cast<const uint2*>(p); }
   __device__ __forceinline__ void clear(int z_x) {   // the code of zero
     v.x = v.y = ((uint32_t)z_x & 0xFFu) * 0x01010101u;
   }
   __device__ __forceinline__ void set(int e, const char* p) {
-    const uint32_t c = (uint32_t)(uint8_t)__ldg(reinterpret_cast<const signed char*>(p));
+    const uint32_t c = (uint32_t)*reinterpret_cast<const uint8_t*>(p);
     uint32_t& w = e < 4 ? v.x : v.y;
     w = (w & ~(0xFFu << (8 * (e & 3)))) | (c << (8 * (e & 3)));
   }
@@ -205,6 +222,15 @@ __device__ __forceinline__ void to_floats(const Input<DT>& in, float (&v)[8]) {
   }
 }
 
+// The inputs of one tile: x[n][i] of row n at `at[n]` + 32 i, inside the row and aligned.
+template <int DT, int NT>
+__device__ __forceinline__ void load_tile(Input<DT> (&x)[NT][4], const char* const (&at)[NT]) {
+#pragma unroll
+  for (int n = 0; n < NT; ++n)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) x[n][i].load(at[n] + 32 * i * Input<DT>::kBytes);
+}
+
 // Inputs k .. k+7 of the row at `row`, the code of zero beyond C.  vec: rows are aligned to eight elements
 // (at most 16 bytes).
 template <int DT>
@@ -221,61 +247,151 @@ __device__ __forceinline__ Input<DT> load_input(const char* row, int k, int C, b
   return in;
 }
 
-// Scales and zeros of the lane's two rows.
-struct RowScales { float s0, s1; uint32_t b0, b1; };
-template <bool F16>
-__device__ __forceinline__ RowScales row_scales(const Packed& w, long tile_K, int grp, int g) {
-  RowScales r;
-  const long at = (tile_K * w.groups + grp) * 16 + g;
-  r.s0 = scale_to_float(__ldg(w.scales + at), w.scale_f16);
-  r.s1 = scale_to_float(__ldg(w.scales + at + 8), w.scale_f16);
-  r.b0 = zero_bias<F16>(w.zeros ? __ldg(w.zeros + at) & 15u : 8u);
-  r.b1 = zero_bias<F16>(w.zeros ? __ldg(w.zeros + at + 8) & 15u : 8u);
-  return r;
+// Codes, scales and zeros of one row tile (16 outputs), from its first input on.
+struct Stream {
+  const uint4* codes;
+  const uint16_t* scales;
+  const uint8_t* zeros;
+};
+__device__ __forceinline__ Stream stream_of(const Packed& w, long tile_K) {
+  return {w.codes + tile_K * w.tiles_C * 64, w.scales + tile_K * w.groups * 16,
+          w.zeros ? w.zeros + tile_K * w.groups * 16 : nullptr};
+}
+
+// A warp's ring of weight tiles in shared memory, filled by asynchronous copies several tiles ahead of
+// their use: each lane copies the two units of codes it will read itself, some lanes the scales and zeros
+// as well (SMALL, groups of 32 or 64 inputs: four or two to a tile; else a group is one or more tiles, and
+// every tile brings its scales along).  A slot holds T consecutive tiles of each of R row tiles.
+template <int R, int T, bool SMALL, bool ZEROS> struct Ring {
+  static constexpr int kGroups = SMALL ? 4 : 1;       // room for, a tile
+  static constexpr int kScales = R * T * 1024, kZeros = kScales + R * T * kGroups * 32;
+  static constexpr int kSlot = kZeros + (ZEROS ? R * T * kGroups * 16 : 0);
+  const char* codes[R];
+  const char* meta[R];     // scales, or zeros, of the row tile
+  int c, end;              // next tile, and the last one's successor
+  int per;                 // groups a tile (SMALL) or tiles a group
+  int groups;
+  // this lane's 16 bytes of scales (two lanes a group) or zeros (a lane a group): tile of the slot, group of
+  // the tile, size of a group, offset in the group, place in the slot; tile >= T: none
+  int my_tile, my_group, my_size, my_part;
+  uint32_t my_place;
+
+  // the next fill is of tiles `from` .. of `w`, none of them `to` or beyond
+  __device__ __forceinline__ void start(const Stream (&w)[R], const Packed& p, int from, int to, int lane) {
+    c = from; end = to; groups = p.groups;
+    per = SMALL ? (p.group == 32 ? 4 : 2) : p.group >> 7;
+    const int of_tile = SMALL ? per : 1;              // groups a tile
+    const bool zero = ZEROS && lane >= 2 * kGroups * T;
+    const int i = zero ? lane - 2 * kGroups * T : lane >> 1;   // group of the slot
+    my_tile = i / of_tile; my_group = i % of_tile;    // powers of two
+    if (!ZEROS && lane >= 2 * kGroups * T) my_tile = T;
+    my_size = zero ? 16 : 32; my_part = zero ? 0 : 16 * (lane & 1);
+    my_place = (zero ? kZeros : kScales) + (my_tile * kGroups + my_group) * my_size + my_part;
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+      codes[r] = reinterpret_cast<const char*>(w[r].codes + c * 64l + lane);
+      meta[r] = (zero ? reinterpret_cast<const char*>(w[r].zeros) : reinterpret_cast<const char*>(w[r].scales)) + my_part;
+    }
+  }
+  __device__ __forceinline__ void fill(uint32_t slot, int lane) {
+    const uint32_t to = slot + lane * 16;
+#pragma unroll
+    for (int j = 0; j < T; ++j)
+      if (j == 0 || c + j < end)
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+          asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to + (r * T + j) * 1024), "l"(codes[r] + j * 1024) : "memory");
+          asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to + (r * T + j) * 1024 + 512), "l"(codes[r] + j * 1024 + 512) : "memory");
+        }
+    const int tile = c + my_tile;
+    const int group = SMALL ? tile * per + my_group : per == 1 ? tile : tile / per;
+    if (my_tile < T && tile < end) {
+      // groups behind the last: zeros in place of what is not there
+      const bool in = !SMALL || group < groups;
+      const int bytes = in ? 16 : 0;
+#pragma unroll
+      for (int r = 0; r < R; ++r)
+        asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(slot + my_place + r * T * kGroups * my_size),
+                     "l"(meta[r] + (in ? group : 0) * (long)my_size), "r"(bytes) : "memory");
+    }
+#pragma unroll
+    for (int r = 0; r < R; ++r) codes[r] += T * 1024;
+    c += T;
+  }
+  __device__ __forceinline__ static void commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+  template <int PENDING> __device__ __forceinline__ static void wait() {
+    asm volatile("cp.async.wait_group %0;" ::"n"(PENDING) : "memory");
+    __syncwarp();
+  }
+};
+
+__device__ __forceinline__ uint32_t lds_u16(uint32_t addr) {
+  uint16_t v;
+  asm volatile("ld.shared.u16 %0, [%1];" : "=h"(v) : "r"(addr));
+  return v;
+}
+__device__ __forceinline__ uint32_t lds_u8(uint32_t addr) {
+  uint32_t v;
+  asm volatile("ld.shared.u8 %0, [%1];" : "=r"(v) : "r"(addr));
+  return v;
+}
+__device__ __forceinline__ uint4 lds_u4(uint32_t addr) {
+  uint4 v;
+  asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(addr));
+  return v;
 }
 
 __device__ __forceinline__ uint32_t word_of(const uint4& u, int i) {
   return i == 0 ? u.x : i == 1 ? u.y : i == 2 ? u.z : u.w;
 }
 
-// One 16 x 128 tile of weights against NT x 8 rows of x: acc += scale * (codes - zeros) x.
-//   SMALL  groups of 32 or 64 inputs (else of a multiple of 128: one sum per tile)
-//   u0, u1: the lane's units of rows g and g + 8;  x[n][i]: the input of row 8 n + g at 32 i + 8 t
-template <bool SMALL, int NT, class In>
-__device__ __forceinline__ void tile_mma(float (&acc)[NT][4], const Packed& w, long tile_K, int tile_C, uint4 u0,
-                                         uint4 u1, const In (&x)[NT][4], int z_x, int g) {
+// One 16 x 128 tile of weights, the one at `index` (r T + j) of a ring's slot, against NT x 8 rows of x: acc +=
+// scale * (codes - zeros) x, the sum of a group multiplied by its scale (for groups of at least 128: of a
+// tile).  x[n][i]: the input of row 8 n + g at 32 i + 8 t.  Two chains of MMAs: one would wait for itself.
+template <bool SMALL, bool ZEROS, class Tiles, int NT, class In>
+__device__ __forceinline__ void tile_mma(float (&acc)[NT][4], uint32_t slot, int index, const Packed& w, const In (&x)[NT][4],
+                                         int z_x, int lane) {
   constexpr bool F16 = In::kF16;
   constexpr int P = In::kParts;
-  RowScales rs;
-  float part[NT][4];
+  const uint32_t tile = slot + index * 1024 + lane * 16;
+  const uint4 u0 = lds_u4(tile), u1 = lds_u4(tile + 512);
+  const uint32_t scales = slot + Tiles::kScales + index * Tiles::kGroups * 32 + (lane >> 2) * 2;
+  const uint32_t zeros = slot + Tiles::kZeros + index * Tiles::kGroups * 16 + (lane >> 2);
+  float part[NT][2][4], s0, s1;
+  uint32_t b0 = zero_bias<F16>(8), b1 = b0;
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     if (SMALL || i == 0) {
-      const int grp = min((int)((tile_C * 128l + 32 * i) / w.group), w.groups - 1);
-      rs = row_scales<F16>(w, tile_K, grp, g);
-#pragma unroll
-      for (int n = 0; n < NT; ++n) part[n][0] = part[n][1] = part[n][2] = part[n][3] = 0.0f;
+      const int grp = SMALL ? (w.group == 32 ? i : i >> 1) : 0;   // a group of 64 counts twice
+      s0 = scale_to_float((uint16_t)lds_u16(scales + grp * 32), w.scale_f16);
+      s1 = scale_to_float((uint16_t)lds_u16(scales + grp * 32 + 16), w.scale_f16);
+      if (ZEROS) {
+        b0 = zero_bias<F16>(lds_u8(zeros + grp * 16) & 15u);
+        b1 = zero_bias<F16>(lds_u8(zeros + grp * 16 + 8) & 15u);
+      }
     }
     uint32_t a0[4], a1[4];
-    unpack8<F16>(word_of(u0, i), rs.b0, a0);
-    unpack8<F16>(word_of(u1, i), rs.b1, a1);
+    unpack8<F16>(word_of(u0, i), b0, a0);
+    unpack8<F16>(word_of(u1, i), b1, a1);
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
       uint32_t b[P][4];
       x[n][i].operand(z_x, b);
 #pragma unroll
       for (int p = P - 1; p >= 0; --p) {
-        mma_16816<F16>(part[n], a0[0], a1[0], a0[1], a1[1], b[p][0], b[p][1]);
-        mma_16816<F16>(part[n], a0[2], a1[2], a0[3], a1[3], b[p][2], b[p][3]);
+        if ((SMALL || i == 0) && p == P - 1) {
+          mma_16816_from_0<F16>(part[n][0], a0[0], a1[0], a0[1], a1[1], b[p][0], b[p][1]);
+          mma_16816_from_0<F16>(part[n][1], a0[2], a1[2], a0[3], a1[3], b[p][2], b[p][3]);
+        } else {
+          mma_16816<F16>(part[n][0], a0[0], a1[0], a0[1], a1[1], b[p][0], b[p][1]);
+          mma_16816<F16>(part[n][1], a0[2], a1[2], a0[3], a1[3], b[p][2], b[p][3]);
+        }
       }
-    }
-    if (SMALL || i == 3) {
-#pragma unroll
-      for (int n = 0; n < NT; ++n) {
-        acc[n][0] = __fmaf_rn(part[n][0], rs.s0, acc[n][0]);
-        acc[n][1] = __fmaf_rn(part[n][1], rs.s0, acc[n][1]);
-        acc[n][2] = __fmaf_rn(part[n][2], rs.s1, acc[n][2]);
-        acc[n][3] = __fmaf_rn(part[n][3], rs.s1, acc[n][3]);
+      if (SMALL || i == 3) {
+        acc[n][0] = __fmaf_rn(__fadd_rn(part[n][0][0], part[n][1][0]), s0, acc[n][0]);
+        acc[n][1] = __fmaf_rn(__fadd_rn(part[n][0][1], part[n][1][1]), s0, acc[n][1]);
+        acc[n][2] = __fmaf_rn(__fadd_rn(part[n][0][2], part[n][1][2]), s1, acc[n][2]);
+        acc[n][3] = __fmaf_rn(__fadd_rn(part[n][0][3], part[n][1][3]), s1, acc[n][3]);
       }
     }
   }
