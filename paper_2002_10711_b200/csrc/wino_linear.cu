@@ -13,17 +13,6 @@ namespace wino {
 
 namespace cg = cooperative_groups;
 
-struct LinearArgs {
-  Packed w;
-  const char* x;
-  long x_row;       // bytes
-  Output out;
-  long y_row;       // elements
-  const float* bias;
-  int M, z_x, vec;
-  int split;        // warps of a block that share a row tile's inputs
-};
-
 constexpr int kRowsWarps = 8;
 #ifndef RING
 #define RING 3
@@ -187,6 +176,9 @@ int launch_type(const LinearArgs& a, int num_sms, cudaStream_t st) {
 }
 
 }  // namespace
+#ifndef TCMIN
+#define TCMIN 9
+#endif
 int launch_linear(const wino_linear_desc_t& d, const void* x, const float* bias, void* y, int num_sms,
                   cudaStream_t st) {
   LinearArgs a;
@@ -205,6 +197,11 @@ int launch_linear(const wino_linear_desc_t& d, const void* x, const float* bias,
   a.out.z_Y = codes ? d.q_Y.zero_point : 0;
   a.out.lo = codes ? (float)(d.q_Y.qmin - d.q_Y.zero_point) : 0.0f;
   a.out.hi = codes ? (float)(d.q_Y.qmax - d.q_Y.zero_point) : 0.0f;
+  if (linear_tc_supported(a, d.x_dtype) && d.M >= TCMIN) {
+    int dev = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess) return WINO_ERR_CUDA;
+    return launch_linear_tc(a, d.x_dtype, num_sms, dev, st);
+  }
   switch (d.x_dtype) {
     case WINO_INT8: return launch_type<WINO_INT8>(a, num_sms, st);
     case WINO_FLOAT: return launch_type<WINO_FLOAT>(a, num_sms, st);

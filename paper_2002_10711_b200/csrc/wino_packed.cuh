@@ -417,4 +417,19 @@ __device__ __forceinline__ void store_output(const Output& o, long at, float sum
   else reinterpret_cast<__half*>(o.y)[at] = __float2half_rn(f);
 }
 
+struct LinearArgs {
+  Packed w;
+  const char* x;
+  long x_row;       // bytes
+  Output out;
+  long y_row;       // elements
+  const float* bias;
+  int M, z_x, vec;
+  int split;        // warps of a block that share a row tile's inputs
+};
+
+// The kernel of wino_linear_tc.cu: bf16 and fp16, rows of x on 16-byte boundaries.
+bool linear_tc_supported(const LinearArgs& a, int x_dtype);
+int launch_linear_tc(const LinearArgs& a, int x_dtype, int num_sms, int device, cudaStream_t st);
+
 }  // namespace wino
