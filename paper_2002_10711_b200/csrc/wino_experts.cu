@@ -15,6 +15,7 @@
 #include <cooperative_groups.h>
 
 #include "wino_packed.cuh"
+#include "wino_spread.h"
 
 namespace wino {
 
@@ -234,7 +235,7 @@ constexpr int kUpDepth = UPRING, kDownDepth = DOWNRING;
 
 // An item is an expert, 8 / split row tiles, and 8 NT of the expert's tokens; a block takes every
 // gridDim.x-th, and has the next one's first tiles on the way while it finishes one.
-template <int DT, int NT, bool SMALL, bool ZEROS>
+template <bool VEC, int DT, int NT, bool SMALL, bool ZEROS>
 __global__ void __launch_bounds__(kExpertWarps * 32)
 k_experts_up(const __grid_constant__ ExpertsArgs a, int split) {
   using In = Input<DT>;
@@ -251,7 +252,6 @@ k_experts_up(const __grid_constant__ ExpertsArgs a, int split) {
   const int part = warp % split;
   const int c0 = (int)((long)a.gate.tiles_C * part / split), c1 = (int)((long)a.gate.tiles_C * (part + 1) / split);
   const uint32_t ring = smem_u32(smem) + warp * kUpDepth * Tiles::kSlot, ring_end = ring + kUpDepth * Tiles::kSlot;
-  const int whole = a.vec ? min(c1, a.D >> 7) : c0;         // tiles inside the rows of x, and aligned
   int slot = blockIdx.x / blocks_K, block_K = blockIdx.x - slot * blocks_K, n0 = 0;
   Tiles tiles;
   auto begin = [&]() {
@@ -272,30 +272,25 @@ k_experts_up(const __grid_constant__ ExpertsArgs a, int split) {
     const int first = lists.first[slot], count = lists.first[slot + 1] - first;
     float acc[2][NT][4];
     const char* row[NT];
-    const char* next[NT];
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
       acc[0][n][0] = acc[0][n][1] = acc[0][n][2] = acc[0][n][3] = 0.0f;
       acc[1][n][0] = acc[1][n][1] = acc[1][n][2] = acc[1][n][3] = 0.0f;
       row[n] = a.x + lists.token[first + min(n0 + 8 * n + g, count - 1)] * a.x_row;
-      next[n] = row[n] + (c0 * 128l + 8 * t) * In::kBytes;
     }
+    In x[NT][4];
+    load_tile<VEC, DT, NT>(x, row, c0, a.D, 0, t);
     uint32_t at = ring;
     for (int c = c0; c < c1; ++c) {
-      In x[NT][4];
-      if (c < whole) {
-        load_tile<DT, NT>(x, next);
-      } else {
+      In now[NT][4];
 #pragma unroll
-        for (int n = 0; n < NT; ++n)
+      for (int n = 0; n < NT; ++n)
 #pragma unroll
-          for (int i = 0; i < 4; ++i) x[n][i] = load_input<DT>(row[n], c * 128 + 32 * i + 8 * t, a.D, a.vec, 0);
-      }
-#pragma unroll
-      for (int n = 0; n < NT; ++n) next[n] += 128 * In::kBytes;
+        for (int i = 0; i < 4; ++i) now[n][i] = x[n][i];
+      load_tile<VEC, DT, NT>(x, row, c + 1, a.D, 0, t);        // one tile ahead
       Tiles::template wait<kUpDepth - 1>();
-      tile_mma<SMALL, ZEROS, Tiles, NT>(acc[0], at, 0, a.gate, x, 0, lane);
-      tile_mma<SMALL, ZEROS, Tiles, NT>(acc[1], at, 1, a.up, x, 0, lane);
+      tile_mma<SMALL, ZEROS, Tiles, NT>(acc[0], at, 0, a.gate, now, 0, lane);
+      tile_mma<SMALL, ZEROS, Tiles, NT>(acc[1], at, 1, a.up, now, 0, lane);
       __syncwarp();            // the slot has been read
       if (c + kUpDepth < c1) tiles.fill(at, lane);
       Tiles::commit();
@@ -321,7 +316,7 @@ k_experts_up(const __grid_constant__ ExpertsArgs a, int split) {
     for (int e = threadIdx.x; e < per_block * NT * 8 * 16; e += kExpertWarps * 32) {
       const int k = e & 15, m = (e >> 4) % (NT * 8), v = (e >> 4) / (NT * 8);
       const int i = (this_K + v) * 16 + k;
-      if (this_n0 + m >= count || i >= a.I) continue;
+      if (this_n0 + m >= count || i >= a.h_row) continue;      // h_row: I rounded up to eight, zeros behind I
       float gs = 0.0f, us = 0.0f;
       for (int w = 0; w < split; ++w) {
         const float* s = sums + ((v * split + w) * NT * 8 + m) * 33 + k;
@@ -330,7 +325,7 @@ k_experts_up(const __grid_constant__ ExpertsArgs a, int split) {
       }
       const float silu = __fdiv_rn(gs, __fadd_rn(1.0f, expf(-gs)));
       const int row_h = first + this_n0 + m;
-      float h = keep_nan(__fmul_rn(__fmul_rn(silu, us), lists.weight[row_h]));
+      float h = i < a.I ? keep_nan(__fmul_rn(__fmul_rn(silu, us), lists.weight[row_h])) : 0.0f;
       uint16_t* to = a.h + row_h * a.h_row + i;
 #pragma unroll
       for (int p = 0; p < P; ++p) {
@@ -391,7 +386,6 @@ k_experts_down(const __grid_constant__ ExpertsArgs a, int split) {
 #pragma unroll
   for (int n = 0; n < NT; ++n) acc[n][0] = acc[n][1] = acc[n][2] = acc[n][3] = 0.0f;
   uint32_t at = ring;
-  const int whole = a.I >> 7;                       // tiles inside the rows of h
   int first = 0, count = 0;
   const uint16_t* row[NT];                          // of h, of the first tokens
   auto row_of = [&](int n) { return a.h + (first + min(n + g, count - 1)) * a.h_row + 8 * t; };
@@ -401,19 +395,12 @@ k_experts_down(const __grid_constant__ ExpertsArgs a, int split) {
     for (int n = 0; n < NT; ++n) row[n] = row_of(8 * n);
   };
   auto load = [&](Planes<P> (&x)[4], const uint16_t* from_h) {
-    if (c < whole) {
 #pragma unroll
-      for (int i = 0; i < 4; ++i)
+    for (int i = 0; i < 4; ++i)
 #pragma unroll
-        for (int p = 0; p < P; ++p) x[i].v[p] = *reinterpret_cast<const uint4*>(from_h + p * a.h_plane + c * 128 + 32 * i);
-    } else {
-#pragma unroll
-      for (int i = 0; i < 4; ++i)
-#pragma unroll
-        for (int p = 0; p < P; ++p)
-          x[i].v[p] = load_input<WINO_BF16>(reinterpret_cast<const char*>(from_h + p * a.h_plane - 8 * t),
-                                            c * 128 + 32 * i + 8 * t, a.I, true, 0).v;
-    }
+      for (int p = 0; p < P; ++p)
+        x[i].v[p] = c * 128 + 32 * i + 8 * t < a.I ? *reinterpret_cast<const uint4*>(from_h + p * a.h_plane + c * 128 + 32 * i)
+                                                   : make_uint4(0, 0, 0, 0);
   };
   if (u0 < u1) enter();
   for (int u = u0; u < u1; ++u) {
@@ -487,6 +474,12 @@ namespace {
 #ifndef DOWNBLOCKS
 #define DOWNBLOCKS 2
 #endif
+// spread_smem for blocks that have Lists in static shared memory besides.
+size_t spread_beside_lists(size_t smem, int per) {
+  const size_t all = spread_smem(smem + sizeof(Lists), per);
+  return all - sizeof(Lists);
+}
+
 // Warps that share one row tile's inputs: a power of two up to `most`, no more warps than there are, and
 // no more than tiles.
 int shared_by(long row_tiles, long tiles, int most, long warps) {
@@ -495,31 +488,33 @@ int shared_by(long row_tiles, long tiles, int most, long warps) {
   return n;
 }
 
-template <int DT, int NT, bool SMALL, bool ZEROS>
+template <bool VEC, int DT, int NT, bool SMALL, bool ZEROS>
 int launch_up(const ExpertsArgs& a, long slots, int num_sms, int dev, cudaStream_t st) {
-  constexpr size_t smem = (size_t)kExpertWarps * (kUpDepth * Ring<2, 1, SMALL, ZEROS>::kSlot + NT * 8 * 33 * sizeof(float));
+  constexpr size_t least = (size_t)kExpertWarps * (kUpDepth * Ring<2, 1, SMALL, ZEROS>::kSlot + NT * 8 * 33 * sizeof(float));
   const long tiles_K = (a.I + 15) / 16;
   const int split = shared_by(tiles_K * slots, a.gate.tiles_C, kExpertWarps, (long)UPBLOCKS * kExpertWarps * num_sms);
   const long items = (tiles_K + kExpertWarps / split - 1) / (kExpertWarps / split) * slots;
-  const long most = (long)UPBLOCKS * num_sms;
+  const long most = (long)UPBLOCKS * num_sms, blocks = items < most ? items : most;
+  const size_t smem = spread_beside_lists(least, (int)((blocks + num_sms - 1) / num_sms));
   static DeviceOnce once;
-  auto kernel = k_experts_up<DT, NT, SMALL, ZEROS>;
-  const int rc = set_max_smem(once, dev, kernel, smem);
+  auto kernel = k_experts_up<VEC, DT, NT, SMALL, ZEROS>;
+  const int rc = set_max_smem(once, dev, kernel, spread_beside_lists(least, 1));
   if (rc != 0) return rc;
-  return launch_kernel(kernel, dim3((unsigned)(items < most ? items : most)), dim3(kExpertWarps * 32), smem, st, true, a, split);
+  return launch_kernel(kernel, dim3((unsigned)blocks), dim3(kExpertWarps * 32), smem, st, true, a, split);
 }
 
 template <int P, int NT, bool SMALL, bool ZEROS>
 int launch_down(const ExpertsArgs& a, long slots, int num_sms, int dev, cudaStream_t st) {
   constexpr size_t ring = (size_t)kExpertWarps * kDownDepth * Ring<1, 1, SMALL, ZEROS>::kSlot;
-  const size_t smem = ring + (size_t)kExpertWarps * a.T * 17 * sizeof(float);
   const long tiles_K = (a.D + 15) / 16;
   const int by = shared_by(tiles_K, (a.I + 127l) / 128 * slots, 8 * kExpertWarps, (long)DOWNBLOCKS * kExpertWarps * num_sms);
   const int split = by < kExpertWarps ? by : kExpertWarps, S = by / split;
   const long blocks = (tiles_K + kExpertWarps / split - 1) / (kExpertWarps / split);
+  const long per_sm = (blocks * S + num_sms - 1) / num_sms;
+  const size_t smem = spread_beside_lists(ring + (size_t)kExpertWarps * a.T * 17 * sizeof(float), per_sm <= 8 ? (int)per_sm : 0);
   static DeviceOnce once;
   auto kernel = k_experts_down<P, NT, SMALL, ZEROS>;
-  const int rc = set_max_smem(once, dev, kernel, ring + (size_t)kExpertWarps * kSliceTokens * 17 * sizeof(float));
+  const int rc = set_max_smem(once, dev, kernel, spread_beside_lists(ring + (size_t)kExpertWarps * kSliceTokens * 17 * sizeof(float), 1));
   if (rc != 0) return rc;
   return launch_kernel_cluster(kernel, dim3((unsigned)(blocks * S)), dim3(kExpertWarps * 32), (unsigned)S, smem, st,
                                true, a, split);
@@ -536,8 +531,11 @@ int launch_slice(const ExpertsArgs& a, int num_sms, cudaStream_t st) {
   int rc = launch_kernel_cluster(k_experts_route<DT>, dim3((unsigned)(a.T * S)), dim3(kRouteThreads), (unsigned)S, 0, st, true, a);
   if (rc != 0) return rc;
   const long slots = (long)a.T * a.top_k < a.E ? (long)a.T * a.top_k : a.E;
-  auto up = a.gate.group < 128 ? (a.gate.zeros ? launch_up<DT, NT, true, true> : launch_up<DT, NT, true, false>)
-                               : (a.gate.zeros ? launch_up<DT, NT, false, true> : launch_up<DT, NT, false, false>);
+  auto up = a.vec && a.D % 8 == 0
+                ? (a.gate.group < 128 ? (a.gate.zeros ? launch_up<true, DT, NT, true, true> : launch_up<true, DT, NT, true, false>)
+                                      : (a.gate.zeros ? launch_up<true, DT, NT, false, true> : launch_up<true, DT, NT, false, false>))
+                : (a.gate.group < 128 ? (a.gate.zeros ? launch_up<false, DT, NT, true, true> : launch_up<false, DT, NT, true, false>)
+                                      : (a.gate.zeros ? launch_up<false, DT, NT, false, true> : launch_up<false, DT, NT, false, false>));
   if ((rc = up(a, slots, num_sms, dev, st)) != 0) return rc;
   auto down = a.down.group < 128 ? (a.down.zeros ? launch_down<P, NT, true, true> : launch_down<P, NT, true, false>)
                                  : (a.down.zeros ? launch_down<P, NT, false, true> : launch_down<P, NT, false, false>);

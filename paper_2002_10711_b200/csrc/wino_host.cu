@@ -596,6 +596,21 @@ DeviceOnce g_once_selftest;
 
 }  // namespace
 
+namespace wino {
+int encode_rows_16bit(CUtensorMap* map, const void* base, bool f16, uint64_t columns, uint64_t rows, uint64_t row_bytes,
+                      uint32_t box_columns, uint32_t box_rows) {
+  EncodeTiledFn fn = get_encode_fn();
+  if (fn == nullptr) return WINO_ERR_CUDA;
+  const cuuint64_t dims[2] = {columns, rows}, strides[1] = {row_bytes};
+  const cuuint32_t box[2] = {box_columns, box_rows}, estr[2] = {1, 1};
+  const CUresult r = fn(map, f16 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2,
+                        const_cast<void*>(base), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                        CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                        CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  return r == CUDA_SUCCESS ? WINO_OK : WINO_ERR_CUDA;
+}
+}  // namespace wino
+
 extern "C" {
 
 int wino_plan(const wino_desc_t* desc, wino_plan_t** out) {

@@ -234,6 +234,10 @@ int launch_mma_peak(int iters, int num_sms, int device, int* status, cudaStream_
 // that nothing arrives at, records WINO_ERR_TIMEOUT in *status and exits normally.
 int launch_wait_probe(long long limit_cycles, int* status, cudaStream_t st);
 
+// Tensor map of rows of 16-bit floats (row_bytes and the base multiples of 16), 128-byte swizzle; zeros outside.
+int encode_rows_16bit(CUtensorMap* map, const void* base, bool f16, uint64_t columns, uint64_t rows, uint64_t row_bytes,
+                      uint32_t box_columns, uint32_t box_rows);
+
 // Layers with 4-bit weights (wino_packed_host.cu checks the arguments).
 int launch_quantize(const wino_packed_t& out, const void* w, int w_dtype, int64_t w_stride, void* values,
                     cudaStream_t st);

@@ -8,24 +8,20 @@
 #include <cooperative_groups.h>
 
 #include "wino_packed.cuh"
+#include "wino_spread.h"
 
 namespace wino {
 
 namespace cg = cooperative_groups;
 
-constexpr int kRowsWarps = 8;
-#ifndef RING
-#define RING 3
-#endif
+constexpr int kRowsWarps = 8, kRowTiles = 2 /* of a warp */, kRingSlots = 3, kMaxCluster = 4;
 
-template <int DT, int NT, int R, bool SMALL, bool ZEROS>
+template <bool VEC, int DT, int NT, bool SMALL, bool ZEROS>
 __global__ void __launch_bounds__(kRowsWarps * 32)
 k_linear_rows(const __grid_constant__ LinearArgs a) {
   using In = Input<DT>;
-  constexpr int T = 2 / R;                           // tiles of inputs a slot
-  using Tiles = Ring<R, T, SMALL, ZEROS>;
-  constexpr int kDepth = RING;
-  constexpr int kSums = R * 16 + 1;                  // floats of a row of sums: one bank apart
+  constexpr int R = kRowTiles, kSums = R * 16 + 1;   // floats of a row of sums: one bank apart
+  using Tiles = Ring<R, 1, SMALL, ZEROS>;
   extern __shared__ __align__(128) uint8_t smem[];
   const cg::cluster_group cluster = cg::this_cluster();
   const int S = (int)cluster.num_blocks(), rank = (int)cluster.block_rank();
@@ -48,42 +44,23 @@ k_linear_rows(const __grid_constant__ LinearArgs a) {
 #pragma unroll
     for (int r = 0; r < R; ++r) w[r] = stream_of(a.w, min(unit * R + r, tiles_K - 1));
     const char* row[NT];
-    const char* next[NT];
 #pragma unroll
-    for (int n = 0; n < NT; ++n) {
-      row[n] = a.x + min(m0 + 8 * n + g, a.M - 1) * a.x_row;
-      next[n] = row[n] + (c0 * 128l + 8 * t) * In::kBytes;
-    }
-    const uint32_t ring = smem_u32(smem) + warp * kDepth * Tiles::kSlot, ring_end = ring + kDepth * Tiles::kSlot;
+    for (int n = 0; n < NT; ++n) row[n] = a.x + min(m0 + 8 * n + g, a.M - 1) * a.x_row;
+    const uint32_t ring = smem_u32(smem) + warp * kRingSlots * Tiles::kSlot, ring_end = ring + kRingSlots * Tiles::kSlot;
     Tiles tiles;
     tiles.start(w, a.w, c0, c1, lane);
 #pragma unroll
-    for (int d = 0; d < kDepth; ++d) {
-      if (c0 + d * T < c1) tiles.fill(ring + d * Tiles::kSlot, lane);
+    for (int d = 0; d < kRingSlots; ++d) {
+      if (c0 + d < c1) tiles.fill(ring + d * Tiles::kSlot, lane);
       Tiles::commit();
     }
-    const int whole = a.vec ? min(c1, a.w.C >> 7) : c0;     // tiles inside the rows of x, and aligned
     uint32_t slot = ring;
-    for (int c = c0; c < c1; c += T) {
+    for (int c = c0; c < c1; ++c) {
+      In x[NT][4];
+      load_tile<VEC, DT, NT>(x, row, c, a.w.C, a.z_x, t);
+      Tiles::template wait<kRingSlots - 1>();
 #pragma unroll
-      for (int j = 0; j < T; ++j) {
-        if (j > 0 && c + j >= c1) break;
-        In x[NT][4];
-        if (c + j < whole) {
-          load_tile<DT, NT>(x, next);
-        } else {
-#pragma unroll
-          for (int n = 0; n < NT; ++n)
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-              x[n][i] = load_input<DT>(row[n], (c + j) * 128 + 32 * i + 8 * t, a.w.C, a.vec, a.z_x);
-        }
-#pragma unroll
-        for (int n = 0; n < NT; ++n) next[n] += 128 * In::kBytes;
-        if (j == 0) Tiles::template wait<kDepth - 1>();
-#pragma unroll
-        for (int r = 0; r < R; ++r) tile_mma<SMALL, ZEROS, Tiles, NT>(acc[r], slot, r * T + j, a.w, x, a.z_x, lane);
-      }
+      for (int r = 0; r < R; ++r) tile_mma<SMALL, ZEROS, Tiles, NT>(acc[r], slot, r, a.w, x, a.z_x, lane);
       __syncwarp();          // the slot has been read
       if (tiles.c < c1) tiles.fill(slot, lane);
       Tiles::commit();
@@ -101,83 +78,88 @@ k_linear_rows(const __grid_constant__ LinearArgs a) {
       for (int e = 0; e < 4; ++e)
         sums[(warp * NT * 8 + 8 * n + 2 * t + (e & 1)) * kSums + r * 16 + g + 8 * (e >> 1)] = acc[r][n][e];
   __syncthreads();
-  // outputs of the block: [unit][row of x][16 R]
-  const int outputs = kRowsWarps / a.split * NT * 8 * R * 16;
-  auto place = [&](int e, int& v, int& m, int& k) {
-    k = e % (R * 16);
-    m = e / (R * 16) % (NT * 8);
-    v = e / (R * 16 * NT * 8);
+  // The block's outputs, 32 of a row of x and unit at a time, lane = output.  Where there is a cluster, block
+  // `rank` finishes its share of them.
+  const int rows = min(NT * 8, a.M - m0), pairs = kRowsWarps / a.split * rows;
+  auto finish = [&](int v, int m, float s) {
+    const long out = ((long)(blockIdx.x / S) * (kRowsWarps / a.split) + v) * 32 + lane;
+    if (out < a.w.K) store_output(a.out, (m0 + m) * a.y_row + out, s, a.bias ? a.bias[out] : 0.0f);
   };
-  auto finish = [&](int v, int m, int k, float s) {
-    const long out = ((long)(blockIdx.x / S) * (kRowsWarps / a.split) + v) * R * 16 + k;
-    if (m0 + m < a.M && out < a.w.K) store_output(a.out, (m0 + m) * a.y_row + out, s, a.bias ? a.bias[out] : 0.0f);
-  };
-  for (int e = threadIdx.x; e < outputs; e += kRowsWarps * 32) {
-    int v, m, k;
-    place(e, v, m, k);
+  for (int e = warp; e < pairs; e += kRowsWarps) {
+    const int v = e / rows, m = e - v * rows;
     float s = 0.0f;
-    for (int i = 0; i < a.split; ++i) s = __fadd_rn(s, sums[((v * a.split + i) * NT * 8 + m) * kSums + k]);
-    if (S > 1) total[(v * NT * 8 + m) * kSums + k] = s;
-    else finish(v, m, k, s);
+    for (int i = 0; i < a.split; ++i) s = __fadd_rn(s, sums[((v * a.split + i) * NT * 8 + m) * kSums + lane]);
+    if (S > 1) total[(v * NT * 8 + m) * kSums + lane] = s;
+    else finish(v, m, s);
   }
   if (S == 1) return;
   cluster.sync();
-  // block `rank` of the cluster finishes its share of the outputs
-  for (int e = threadIdx.x * S + rank; e < outputs; e += kRowsWarps * 32 * S) {
-    int v, m, k;
-    place(e, v, m, k);
-    float s = 0.0f;
-    for (int b = 0; b < S; ++b) s = __fadd_rn(s, cluster.map_shared_rank(total, b)[(v * NT * 8 + m) * kSums + k]);
-    finish(v, m, k, s);
+  for (int e = warp * S + rank; e < pairs; e += kRowsWarps * S) {
+    const int v = e / rows, m = e - v * rows;
+    float s = 0.0f, part_of[kMaxCluster];
+#pragma unroll
+    for (int b = 0; b < kMaxCluster; ++b)
+      part_of[b] = b < S ? cluster.map_shared_rank(total, b)[(v * NT * 8 + m) * kSums + lane] : 0.0f;
+#pragma unroll
+    for (int b = 0; b < kMaxCluster; ++b) s = __fadd_rn(s, part_of[b]);
+    finish(v, m, s);
   }
   cluster.sync();   // no block leaves while another reads its sums
 }
 
 namespace {
 
-#ifndef WARPS_PER_SM
-#define WARPS_PER_SM 16
-#endif
-template <int DT, int NT, int R, bool SMALL, bool ZEROS>
+template <bool VEC, int DT, int NT, bool SMALL, bool ZEROS>
 int launch_rows(const LinearArgs& given, int num_sms, cudaStream_t st) {
   LinearArgs a = given;
-  const long units = ((a.w.K + 15) / 16 + R - 1) / R, slices = (a.M + NT * 8 - 1) / (NT * 8);
+  const long units = ((a.w.K + 15) / 16 + kRowTiles - 1) / kRowTiles, slices = (a.M + NT * 8 - 1) / (NT * 8);
   if (slices > 65535) return WINO_ERR_UNSUPPORTED;
-  // inputs shared by as many warps as it takes to have WARPS_PER_SM of them on every SM
-  int shared_by = 1;
-  while (shared_by < 64 && units * slices * shared_by < (long)WARPS_PER_SM * num_sms && shared_by * 2 <= a.w.tiles_C) shared_by *= 2;
-  a.split = shared_by < kRowsWarps ? shared_by : kRowsWarps;
-  const int S = shared_by / a.split;
+  // Inputs shared by as many warps as two blocks an SM have: split of a block times S of a cluster.
+  const long room = 2l * kRowsWarps * num_sms;
+  int S = 1, best = 0;
+  a.split = 1;
+  for (int split = 1; split <= kRowsWarps; split *= 2)
+    for (int s = 1; s <= kMaxCluster; ++s) {
+      const int by = split * s;
+      if (by > 1 && (units * slices * by > room || by > a.w.tiles_C)) break;
+      if (by > best || (by == best && s < S)) best = by, S = s, a.split = split;
+    }
   const long blocks = (units + kRowsWarps / a.split - 1) / (kRowsWarps / a.split);
   const dim3 grid((unsigned)(blocks * S), (unsigned)slices);
-  constexpr int kDepth = RING;
-  constexpr size_t ring = (size_t)kRowsWarps * kDepth * Ring<R, 2 / R, SMALL, ZEROS>::kSlot;
-  constexpr size_t sums = (size_t)2 * kRowsWarps * NT * 8 * (R * 16 + 1) * sizeof(float);
-  constexpr size_t smem = ring > sums ? ring : sums;
-  auto kernel = k_linear_rows<DT, NT, R, SMALL, ZEROS>;
+  constexpr size_t ring = (size_t)kRowsWarps * kRingSlots * Ring<kRowTiles, 1, SMALL, ZEROS>::kSlot;
+  constexpr size_t sums = (size_t)2 * kRowsWarps * NT * 8 * (kRowTiles * 16 + 1) * sizeof(float);
+  constexpr size_t least = ring > sums ? ring : sums;
+  // no more blocks on an SM than its share: while the kernel in front runs they would gather on a few
+  const long per_sm = (blocks * S * slices + num_sms - 1) / num_sms;
+  const size_t smem = spread_smem(least, per_sm <= 8 ? (int)per_sm : 0);
+  auto kernel = k_linear_rows<VEC, DT, NT, SMALL, ZEROS>;
   static DeviceOnce once;
   int dev = 0;
   if (cudaGetDevice(&dev) != cudaSuccess) return WINO_ERR_CUDA;
-  const int rc = set_max_smem(once, dev, kernel, smem);
+  const int rc = set_max_smem(once, dev, kernel, spread_smem(least, 1));
   if (rc != 0) return rc;
   return launch_kernel_cluster(kernel, grid, dim3(kRowsWarps * 32), (unsigned)S, smem, st, true, a);
 }
 
-template <int DT, int NT, int R>
+template <bool VEC, int DT, int NT>
 int launch_groups(const LinearArgs& a, int num_sms, cudaStream_t st) {
   if (a.w.zeros != nullptr)
-    return a.w.group < 128 ? launch_rows<DT, NT, R, true, true>(a, num_sms, st) : launch_rows<DT, NT, R, false, true>(a, num_sms, st);
-  return a.w.group < 128 ? launch_rows<DT, NT, R, true, false>(a, num_sms, st) : launch_rows<DT, NT, R, false, false>(a, num_sms, st);
+    return a.w.group < 128 ? launch_rows<VEC, DT, NT, true, true>(a, num_sms, st)
+                           : launch_rows<VEC, DT, NT, false, true>(a, num_sms, st);
+  return a.w.group < 128 ? launch_rows<VEC, DT, NT, true, false>(a, num_sms, st)
+                         : launch_rows<VEC, DT, NT, false, false>(a, num_sms, st);
 }
 
 template <int DT>
 int launch_type(const LinearArgs& a, int num_sms, cudaStream_t st) {
-  return a.M <= 8 ? launch_groups<DT, 1, 1>(a, num_sms, st) : launch_groups<DT, 2, 2>(a, num_sms, st);
+  if (a.vec && a.w.C % 8 == 0)
+    return a.M <= 8 ? launch_groups<true, DT, 1>(a, num_sms, st) : launch_groups<true, DT, 2>(a, num_sms, st);
+  return launch_groups<false, DT, 1>(a, num_sms, st);
 }
 
 }  // namespace
 #ifndef TCMIN
-#define TCMIN 9
+#define TCMIN 17
 #endif
 int launch_linear(const wino_linear_desc_t& d, const void* x, const float* bias, void* y, int num_sms,
                   cudaStream_t st) {

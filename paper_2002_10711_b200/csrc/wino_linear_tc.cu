@@ -7,15 +7,18 @@
 // multiplied by the output's scale into 32-bit sums in registers: no weight is rounded.
 //
 //   warps 0-3    epilogue: lane = output; slot -> registers, times the scale, added up
-//   warps 4-11   two sets that take chunks in turn: copies of codes and of x several chunks ahead, unpacking;
-//                warp w of a set fills lanes 32 (w % 4) .. +31
-//   warp 12      tensor-memory owner; issues the MMAs
+//   then kSets sets of four warps that take chunks in turn: copies of codes several chunks ahead, unpacking
+//                into the set's buffer of tensor memory; warp w of a set fills lanes 32 (w % 4) .. +31
+//   then a warp that owns the tensor memory and issues the MMAs, and one whose leader copies x by TMA
 //
+// What bounds it is the unpacking (seven instructions of the ALU pipe for eight codes), which is why sixteen
+// of the 22 warps do it, and why x, which needs no conversion, is left to the copy engine.
 // Codes are copied in the order they are stored (512 consecutive bytes an instruction) to places in which a
 // lane finds the four units of its own row without bank conflicts: unit t of row r stands at
 // t ^ (r / 2 % 4).  The blocks of a cluster share the inputs and add their sums in a fixed order.
 #include <cooperative_groups.h>
 
+#include "wino_f32x2.cuh"
 #include "wino_packed.cuh"
 
 namespace wino {
@@ -24,16 +27,29 @@ namespace cg = cooperative_groups;
 
 namespace {
 
-constexpr int kTcThreads = 13 * 32, kTcStages = 3 /* code stages of a set */, kTcA = 2 /* A buffers */;
+#ifndef SETS
+#define SETS 4
+#endif
+#ifndef CSTAGES
+#define CSTAGES 3
+#endif
+#ifndef XSTAGES
+#define XSTAGES 4
+#endif
+constexpr int kSets = SETS, kTcStages = CSTAGES /* code stages of a set */, kXStages = XSTAGES /* chunks of x */;
+constexpr int kMmaWarp = 4 + 4 * kSets, kXWarp = kMmaWarp + 1, kTcThreads = (kXWarp + 1) * 32;
 
-__device__ __forceinline__ void mma_f16_ts(uint32_t d, uint32_t a, uint64_t bdesc, uint32_t idesc, uint32_t accumulate) {
+template <bool ACCUMULATE>
+__device__ __forceinline__ void mma_f16_ts(uint32_t d, uint32_t a, uint32_t bdesc_lo, uint32_t bdesc_hi, uint32_t idesc) {
   asm volatile(
       "{\n"
       ".reg .pred p;\n"
-      "setp.ne.b32 p, %4, 0;\n"
-      "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n"
+      ".reg .b64 b;\n"
+      "mov.b64 b, {%2, %3};\n"
+      "setp.ne.b32 p, %5, 0;\n"
+      "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], b, %4, p;\n"
       "}\n"
-      ::"r"(d), "r"(a), "l"(bdesc), "r"(idesc), "r"(accumulate)
+      ::"r"(d), "r"(a), "r"(bdesc_lo), "r"(bdesc_hi), "r"(idesc), "n"(ACCUMULATE ? 1 : 0)
       : "memory");
 }
 __device__ __forceinline__ void tmem_st32(uint32_t taddr, const uint32_t (&r)[32]) {
@@ -55,29 +71,31 @@ constexpr uint32_t idesc_f16(bool f16, int M, int N) {
   return (1u << 4) | (f16 ? 0u : (1u << 7) | (1u << 10)) | ((uint32_t)(N >> 3) << 17) | ((uint32_t)(M >> 4) << 24);
 }
 
-struct TcShape {
-  // chunks whose x is on the way or in use: copies run 2 kTcStages chunks ahead of the MMA at most kTcA behind
-  static constexpr int kB = 2 * kTcStages + kTcA;
-};
 constexpr int tc_columns(int NP, int slots) {
   int n = 32;
-  while (n < kTcA * 64 + slots * NP) n *= 2;
+  while (n < kSets * 64 + slots * NP) n *= 2;
   return n;
 }
-// Slots of sums: four while they fit beside the A buffers.
-constexpr int tc_slots(int NP) { return NP <= 64 ? 4 : 3; }
+constexpr int kSlots = 4;   // of sums
+constexpr int kScaleStages = 8;
+// A stage of codes: 128 rows of 64 bytes, and zeros [4 warps][2 row tiles][4 groups][16].
+constexpr uint32_t kZerosAt = 8192, kStageBytes = 8192 + 512;
 
-struct TcBars { uint64_t a_full[kTcA], a_empty[kTcA], d_full[4], d_empty[4]; uint32_t tmem, abort; };
+struct TcBars {
+  uint64_t a_full[kSets], a_empty[kSets], d_full[kSlots], d_empty[kSlots], x_full[kXStages], x_empty[kXStages];
+  uint32_t tmem, abort;
+};
 
 template <bool F16, int NP, bool SMALL, bool ZEROS>
-__global__ void __launch_bounds__(kTcThreads, NP <= 16 ? 2 : 1)
-k_linear_tc(const __grid_constant__ LinearArgs a, int* __restrict__ status) {
-  constexpr int kSlots = tc_slots(NP), kB = TcShape::kB, kColumns = tc_columns(NP, kSlots);
-  constexpr uint32_t kBytesB = NP * 256, kHalfB = NP * 128;      // a chunk of x: two halves of 64 inputs
+__global__ void __launch_bounds__(kTcThreads, 1)
+k_linear_tc(const __grid_constant__ LinearArgs a, const __grid_constant__ CUtensorMap map_x, int* __restrict__ status) {
+  constexpr int kColumns = tc_columns(NP, kSlots);
+  constexpr uint32_t kBytesX = NP * 256, kHalfX = NP * 128;      // a chunk of x: two halves of 64 inputs
   extern __shared__ uint8_t smem_raw[];
   __shared__ TcBars bars;
   const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
-  const uint32_t ring_codes = base + kB * kBytesB;               // [set][stage][128 rows][64 bytes]
+  const uint32_t ring_codes = base + kXStages * kBytesX;         // [set][stage]
+  const uint32_t scales_at = ring_codes + kSets * kTcStages * kStageBytes;   // [warp][stage][2 row tiles][16]
   const cg::cluster_group cluster = cg::this_cluster();
   const int S = (int)cluster.num_blocks(), rank = (int)cluster.block_rank();
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -87,7 +105,7 @@ k_linear_tc(const __grid_constant__ LinearArgs a, int* __restrict__ status) {
   volatile uint32_t* abort_p = &bars.abort;
 
   if (threadIdx.x == 0) {
-    for (int i = 0; i < kTcA; ++i) {
+    for (int i = 0; i < kSets; ++i) {
       mbar_init(smem_u32(&bars.a_full[i]), 4);
       mbar_init(smem_u32(&bars.a_empty[i]), 1);
     }
@@ -95,258 +113,268 @@ k_linear_tc(const __grid_constant__ LinearArgs a, int* __restrict__ status) {
       mbar_init(smem_u32(&bars.d_full[i]), 1);
       mbar_init(smem_u32(&bars.d_empty[i]), 4);
     }
+    for (int i = 0; i < kXStages; ++i) {
+      mbar_init(smem_u32(&bars.x_full[i]), 1);
+      mbar_init(smem_u32(&bars.x_empty[i]), 1);
+    }
     bars.abort = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    tma_prefetch_map(&map_x);
   }
   // Tensor memory is taken when the kernel in front is over, and the next may start when it is taken: no
   // block holds some while it waits for one that needs some.
   griddep_wait();
-  if (warp == 12) tmem_alloc(smem_u32(&bars.tmem), kColumns);
+  if (warp == kMmaWarp) tmem_alloc(smem_u32(&bars.tmem), kColumns);
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
   griddep_launch();
-  const uint32_t tmem = bars.tmem, tmem_d = tmem + kTcA * 64;
+  const uint32_t tmem = bars.tmem, tmem_d = tmem + kSets * 64;
 
-  float acc[NP];                                                 // epilogue only
+  F2 acc[NP / 2];                                                // epilogue only: rows of x 2 i, 2 i + 1
   if (warp < 4) {
 #pragma unroll
-    for (int i = 0; i < NP; ++i) acc[i] = 0.0f;
-    // this lane's output among the packed rows, and its scales, fetched eight sums ahead
-    const long row_tile = min(block_K * 8 + warp * 2 + (lane >> 4), tiles_K - 1);
-    const uint16_t* scales = a.w.scales + row_tile * a.w.groups * 16 + (lane & 15);
+    for (int i = 0; i < NP / 2; ++i) acc[i] = f2_both(0.0f);
+    // Scales of the warp's two row tiles, 64 bytes a sum, copied kScaleStages sums ahead by lanes 0 .. 3.  (Held in
+    // registers they would be waited for wherever a register is moved.)
+    const long row_tile = min(block_K * 8 + warp * 2 + (lane >> 1 & 1), tiles_K - 1);
+    const char* from_scales = reinterpret_cast<const char*>(a.w.scales + row_tile * a.w.groups * 16) + (lane & 1) * 16;
+    const uint32_t ring = scales_at + warp * kScaleStages * 64;
     const int per = SMALL ? 1 : a.w.group >> 7, all = n * parts;
-    auto scale = [&](int i) -> uint32_t {
-      if (i >= all) return 0;
-      const int grp = SMALL ? first * parts + i : per == 1 ? first + i : (first + i) / per;
-      return scales[min(grp, a.w.groups - 1) * 16l];
-    };
-    uint32_t next[8];
-#pragma unroll
-    for (int i = 0; i < 8; ++i) next[i] = scale(i);
-    bool ok = true;
-    int slot = 0;
-    uint32_t phase = 0;
-    for (int i0 = 0; i0 < all && ok; i0 += 8) {
-#pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        if (i0 + j >= all || !ok) break;
-        const float s = scale_to_float((uint16_t)next[j], a.w.scale_f16);
-        next[j] = scale(i0 + j + 8);
-        ok = __all_sync(0xffffffffu, mbar_wait<false>(smem_u32(&bars.d_full[slot]), phase, abort_p));
-        if (!ok) break;
-        tc_fence_after();
-        const uint32_t from = tmem_d + slot * NP + ((uint32_t)(warp * 32) << 16);
-        if constexpr (NP == 16) {
-          uint32_t d[16];
-          tmem_ld16(from, d);
-          tmem_ld_wait();
-          tc_fence_before();
-          __syncwarp();
-          if (lane == 0) mbar_arrive(smem_u32(&bars.d_empty[slot]));
-#pragma unroll
-          for (int i = 0; i < 16; ++i) acc[i] = __fmaf_rn(__uint_as_float(d[i]), s, acc[i]);
-        } else {
-#pragma unroll
-          for (int col = 0; col < NP; col += 32) {
-            uint32_t d[32];
-            tmem_ld32(from + col, d);
-            tmem_ld_wait();
-            if (col + 32 == NP) {
-              tc_fence_before();
-              __syncwarp();
-              if (lane == 0) mbar_arrive(smem_u32(&bars.d_empty[slot]));
-            }
-#pragma unroll
-            for (int i = 0; i < 32; ++i) acc[col + i] = __fmaf_rn(__uint_as_float(d[i]), s, acc[col + i]);
-          }
-        }
-        if (++slot == kSlots) slot = 0, phase ^= 1u;
-      }
-    }
-    if (!ok) *abort_p = 1u;
-  } else if (warp < 12) {
-    const int set = (warp - 4) >> 2, quad = warp & 3, u = threadIdx.x - 128 - set * 128;
-    const uint32_t codes_at = ring_codes + set * kTcStages * 8192 + quad * 2048;
-    // copies: instruction k takes rows 8 k .. 8 k + 7 of the warp's 32
-    const uint32_t to = (uint32_t)((lane >> 2) * 64 + (((lane & 3) ^ (lane >> 3 & 3)) << 4));
-    const long tile0 = min(block_K * 8 + quad * 2, tiles_K - 1), tile1 = min(block_K * 8 + quad * 2 + 1, tiles_K - 1);
-    const uint4* from0 = a.w.codes + tile0 * a.w.tiles_C * 64 + lane;
-    const uint4* from1 = a.w.codes + tile1 * a.w.tiles_C * 64 + lane;
-    // x: rows u / 16 + 8 k, piece u % 16 of 16 bytes of a chunk's row
-    const int xr = u >> 4, piece = u & 15;
-    const uint32_t x_to = base + (piece >> 3) * kHalfB + xr * 128 + (((piece & 7) ^ xr) << 4);
-    const char* x_from = a.x + (long)(m0 + xr) * a.x_row + piece * 16;
-    auto copy = [&](int q, int stage) {
-      if (q < n) {
-        const long c = first + q;
-        const uint32_t s = codes_at + stage * 8192 + to;
-        asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(s), "l"(from0 + c * 64) : "memory");
-        asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(s + 512), "l"(from0 + c * 64 + 32) : "memory");
-        asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(s + 1024), "l"(from1 + c * 64) : "memory");
-        asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(s + 1536), "l"(from1 + c * 64 + 32) : "memory");
-        const uint32_t b = x_to + (q % kB) * kBytesB;
-        const int left = (a.w.C - (int)c * 128 - piece * 8) * 2;     // bytes of the row from this piece on
-        const int bytes = left < 0 ? 0 : left > 16 ? 16 : left;
-        const char* x = bytes > 0 ? x_from + c * 256 : a.x;
-#pragma unroll
-        for (int k = 0; k < NP / 8; ++k)
-          if (m0 + xr + 8 * k < a.M)
-            asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(b + k * 1024), "l"(x + (bytes > 0 ? 8l * k * a.x_row : 0l)), "r"(bytes) : "memory");
+    auto copy = [&](int i) {
+      if (i < all && lane < 4) {
+        const int grp = SMALL ? first * parts + i : per == 1 ? first + i : (first + i) / per;
+        asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(ring + (i % kScaleStages) * 64 + lane * 16),
+                     "l"(from_scales + min(grp, a.w.groups - 1) * 32l) : "memory");
       }
       asm volatile("cp.async.commit_group;" ::: "memory");
     };
-    // zeros of this lane's row: up to four of a chunk, a byte each
-    const uint8_t* zeros = ZEROS ? a.w.zeros + (lane < 16 ? tile0 : tile1) * a.w.groups * 16 + (lane & 15) : nullptr;
-    auto zero = [&](int q) -> uint32_t {
-      if (!ZEROS || q >= n) return 0;
-      uint32_t z = 0;
-      if constexpr (SMALL) {
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-          if (i < parts) z |= (uint32_t)zeros[min((first + q) * parts + i, a.w.groups - 1) * 16l] << (8 * i);
-      } else {
-        const int per = a.w.group >> 7;
-        z = zeros[(per == 1 ? first + q : (first + q) / per) * 16l];
-      }
-      return z;
-    };
-    uint32_t z[kTcStages];
-#pragma unroll
-    for (int d = 0; d < kTcStages; ++d) {
-      copy(set + 2 * d, d);
-      z[d] = zero(set + 2 * d);
-    }
-    const uint32_t row_at = codes_at + lane * 64, swap = (uint32_t)(lane >> 1 & 3) << 4;
+    for (int i = 0; i < kScaleStages; ++i) copy(i);
     bool ok = true;
-    for (int q0 = set; q0 < n && ok; q0 += 2 * kTcStages) {
+    int slot = 0;
+    uint32_t phase = 0;
+    for (int i = 0; i < all; ++i) {
+      asm volatile("cp.async.wait_group %0;" ::"n"(kScaleStages - 1) : "memory");
+      __syncwarp();
+      const F2 s = f2_both(scale_to_float((uint16_t)lds_u16(ring + (i % kScaleStages) * 64 + lane * 2), a.w.scale_f16));
+      ok = __all_sync(0xffffffffu, mbar_wait<false>(smem_u32(&bars.d_full[slot]), phase, abort_p));
+      if (!ok) break;
+      copy(i + kScaleStages);            // every lane has read its scale
+      tc_fence_after();
+      const uint32_t from = tmem_d + slot * NP + ((uint32_t)(warp * 32) << 16);
 #pragma unroll
-      for (int d = 0; d < kTcStages; ++d) {
-        const int q = q0 + 2 * d;
-        if (q >= n || !ok) break;
-        asm volatile("cp.async.wait_group %0;" ::"n"(kTcStages - 1) : "memory");
-        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");     // x is read by the MMA
-        __syncwarp();
-        uint4 c[4];
-#pragma unroll
-        for (int t = 0; t < 4; ++t) c[t] = lds_u4(row_at + d * 8192 + ((uint32_t)(t << 4) ^ swap));
-        const int buf = q % kTcA;
-        ok = __all_sync(0xffffffffu, mbar_wait<false>(smem_u32(&bars.a_empty[buf]), ((q / kTcA) & 1) ^ 1, abort_p));
-        if (!ok) break;
-        tc_fence_after();
-        const uint32_t a_at = tmem + buf * 64 + ((uint32_t)(quad * 32) << 16);
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          uint32_t r[32];
-#pragma unroll
-          for (int i = 0; i < 2; ++i) {
-            uint32_t bias = zero_bias<F16>(8);
-            if (ZEROS) bias = zero_bias<F16>((SMALL ? z[d] >> (8 * (parts == 4 ? 2 * h + i : h)) : z[d]) & 15u);
-#pragma unroll
-            for (int t = 0; t < 4; ++t) {
-              uint32_t v[4];
-              unpack8<F16>(word_of(c[t], 2 * h + i), bias, v);
-#pragma unroll
-              for (int p = 0; p < 4; ++p) r[i * 16 + t * 4 + p] = v[p];
-            }
-          }
-          tmem_st32(a_at + h * 32, r);
+      for (int col = 0; col < NP; col += 16) {
+        uint32_t d[16];
+        tmem_ld16(from + col, d);
+        tmem_ld_wait();
+        if (col + 16 == NP) {
+          tc_fence_before();
+          __syncwarp();
+          if (lane == 0) mbar_arrive(smem_u32(&bars.d_empty[slot]));
         }
-        tmem_st_wait();
-        tc_fence_before();
-        __syncwarp();
-        if (lane == 0) mbar_arrive(smem_u32(&bars.a_full[buf]));
-        copy(q + 2 * kTcStages, d);
-        z[d] = zero(q + 2 * kTcStages);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) acc[col / 2 + e] = v_fma(f2_bits(d[2 * e], d[2 * e + 1]), s, acc[col / 2 + e]);
       }
+      if (++slot == kSlots) slot = 0, phase ^= 1u;
     }
     if (!ok) *abort_p = 1u;
     asm volatile("cp.async.wait_all;" ::: "memory");
-  } else {
-    const bool leader = elect_one();
-    constexpr uint32_t idesc = idesc_f16(F16, 128, NP);
-    const int steps = 8 / parts;                                 // MMAs a sum
-    bool ok = true;
-    int slot = 0;
-    uint32_t phase = 1;
-    for (int q = 0; q < n; ++q) {
-      const int buf = q % kTcA;
-      if (!(ok = __all_sync(0xffffffffu, mbar_wait<false>(smem_u32(&bars.a_full[buf]), (q / kTcA) & 1, abort_p)))) break;
-      tc_fence_after();
-      const uint64_t desc = make_desc_sw128(base + (q % kB) * kBytesB);
-      for (int p = 0; p < parts; ++p) {
-        if (!(ok = __all_sync(0xffffffffu, mbar_wait<false>(smem_u32(&bars.d_empty[slot]), phase, abort_p)))) break;
-        tc_fence_after();
-        if (leader) {
-          for (int s = 0; s < steps; ++s) {
-            const int k = p * steps + s;                         // inputs 16 k .. +15
-            mma_f16_ts(tmem_d + slot * NP, tmem + buf * 64 + k * 8, desc + (uint64_t)((k >> 2) * (kHalfB >> 4) + (k & 3) * 2),
-                       idesc, s > 0 ? 1u : 0u);
-          }
-          mma_commit(smem_u32(&bars.d_full[slot]));
-          if (p + 1 == parts) mma_commit(smem_u32(&bars.a_empty[buf]));
+  } else if (warp < kMmaWarp) {
+    const int set = (warp - 4) >> 2, quad = warp & 3;
+    const uint32_t ring = ring_codes + set * kTcStages * kStageBytes, codes_at = ring + quad * 2048, zeros_at = ring + kZerosAt + quad * 128;
+    // copies: instruction k takes rows 8 k .. 8 k + 7 of the warp's 32
+    const uint32_t to = (uint32_t)((lane >> 2) * 64 + (((lane & 3) ^ (lane >> 3 & 3)) << 4));
+    const long tile0 = min(block_K * 8 + quad * 2, tiles_K - 1), tile1 = min(block_K * 8 + quad * 2 + 1, tiles_K - 1);
+    const uint4* from0 = a.w.codes + (tile0 * a.w.tiles_C + first + set) * 64 + lane;
+    const uint4* from1 = a.w.codes + (tile1 * a.w.tiles_C + first + set) * 64 + lane;
+    // zeros: 16 bytes of row tile lane / 4 and group lane % 4 of the chunk
+    const uint8_t* from_zeros = ZEROS ? a.w.zeros + (lane < 4 ? tile0 : tile1) * a.w.groups * 16 : nullptr;
+    int ahead = set;                                             // the chunk that is copied next
+    auto copy = [&](uint32_t stage) {
+      if (ahead < n) {
+        const uint32_t s = codes_at + stage + to;
+        asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(s), "l"(from0) : "memory");
+        asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(s + 512), "l"(from0 + 32) : "memory");
+        asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(s + 1024), "l"(from1) : "memory");
+        asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(s + 1536), "l"(from1 + 32) : "memory");
+        if (ZEROS && lane < 8 && (lane & 3) < parts) {
+          const int per = SMALL ? 1 : a.w.group >> 7;
+          const int grp = SMALL ? (first + ahead) * parts + (lane & 3) : per == 1 ? first + ahead : (first + ahead) / per;
+          asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(zeros_at + stage + lane * 16),
+                       "l"(from_zeros + min(grp, a.w.groups - 1) * 16l) : "memory");
         }
-        __syncwarp();
-        if (++slot == kSlots) slot = 0, phase ^= 1u;
+        from0 += 64 * kSets; from1 += 64 * kSets;
+        ahead += kSets;
+      }
+      asm volatile("cp.async.commit_group;" ::: "memory");
+    };
+    for (int d = 0; d < kTcStages; ++d) copy(d * kStageBytes);
+    const uint32_t row_at = codes_at + lane * 64, swap = (uint32_t)(lane >> 1 & 3) << 4;
+    const uint32_t a_at = tmem + set * 64 + ((uint32_t)(quad * 32) << 16);
+    const uint32_t full = smem_u32(&bars.a_full[set]), empty = smem_u32(&bars.a_empty[set]);
+    bool ok = true;
+    uint32_t stage = 0, phase = 1;
+    for (int q = set; q < n; q += kSets) {
+      asm volatile("cp.async.wait_group %0;" ::"n"(kTcStages - 1) : "memory");
+      __syncwarp();
+      uint4 c[4];
+#pragma unroll
+      for (int t = 0; t < 4; ++t) c[t] = lds_u4(row_at + stage + ((uint32_t)(t << 4) ^ swap));
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        uint32_t r[32];
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          uint32_t bias = zero_bias<F16>(8);
+          if (ZEROS) bias = zero_bias<F16>(lds_u8(zeros_at + stage + (lane >> 4) * 64 + (SMALL ? (parts == 4 ? 2 * h + i : h) : 0) * 16 + (lane & 15)) & 15u);
+#pragma unroll
+          for (int t = 0; t < 4; ++t) {
+            uint32_t v[4];
+            unpack8<F16>(word_of(c[t], 2 * h + i), bias, v);
+#pragma unroll
+            for (int p = 0; p < 4; ++p) r[i * 16 + t * 4 + p] = v[p];
+          }
+        }
+        if (h == 0) {
+          ok = __all_sync(0xffffffffu, mbar_wait<false>(empty, phase, abort_p));
+          if (!ok) break;
+          tc_fence_after();
+        }
+        tmem_st32(a_at + h * 32, r);
       }
       if (!ok) break;
+      __syncwarp();
+      copy(stage);                        // every lane has read its part
+      tmem_st_wait();
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(full);
+      phase ^= 1u;
+      stage = stage == (kTcStages - 1) * kStageBytes ? 0 : stage + kStageBytes;
     }
-    // the last commit has arrived
-    ok = ok && __all_sync(0xffffffffu, mbar_wait<false>(smem_u32(&bars.a_empty[(n - 1) % kTcA]), ((n - 1) / kTcA) & 1, abort_p));
     if (!ok) *abort_p = 1u;
+    asm volatile("cp.async.wait_all;" ::: "memory");
+  } else if (warp == kMmaWarp) {
+    // One thread: what it does between two chunks is what a chunk takes at least, so its MMAs are laid out in a
+    // row and it waits for no other lane.
+    if (elect_one()) {
+      constexpr uint32_t idesc = idesc_f16(F16, 128, NP);
+      const uint64_t desc0 = make_desc_sw128(base);
+      const uint32_t desc_hi = (uint32_t)(desc0 >> 32);
+      bool ok = true;
+      int slot = 0, set = 0, xs = 0;
+      uint32_t d_phase = 1, a_phase = 0, x_phase = 0;
+      for (int q = 0; q < n; ++q) {
+        if (!(ok = mbar_wait<false>(smem_u32(&bars.x_full[xs]), x_phase, abort_p))) break;
+        if (!(ok = mbar_wait<false>(smem_u32(&bars.a_full[set]), a_phase, abort_p))) break;
+        const uint32_t desc = (uint32_t)desc0 + xs * (kBytesX >> 4), from = tmem + set * 64;
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {                            // inputs 16 k .. +15
+          const bool begins = SMALL ? k % (parts == 4 ? 2 : 4) == 0 : k == 0;
+          const bool ends = SMALL ? k % (parts == 4 ? 2 : 4) == (parts == 4 ? 1 : 3) : k == 7;
+          if (begins) {
+            if (!(ok = mbar_wait<false>(smem_u32(&bars.d_empty[slot]), d_phase, abort_p))) break;
+            tc_fence_after();
+          }
+          const uint32_t d = tmem_d + slot * NP, b = desc + (k >> 2) * (kHalfX >> 4) + (k & 3) * 2;
+          if (begins) mma_f16_ts<false>(d, from + k * 8, b, desc_hi, idesc);
+          else mma_f16_ts<true>(d, from + k * 8, b, desc_hi, idesc);
+          if (ends) {
+            mma_commit(smem_u32(&bars.d_full[slot]));
+            if (++slot == kSlots) slot = 0, d_phase ^= 1u;
+          }
+        }
+        if (!ok) break;
+        mma_commit(smem_u32(&bars.a_empty[set]));
+        mma_commit(smem_u32(&bars.x_empty[xs]));
+        if (++set == kSets) set = 0, a_phase ^= 1u;
+        if (++xs == kXStages) xs = 0, x_phase ^= 1u;
+      }
+      // the last commit has arrived (commits arrive in order)
+      ok = ok && mbar_wait<false>(smem_u32(&bars.x_empty[(n - 1) % kXStages]), ((n - 1) / kXStages) & 1, abort_p);
+      if (!ok) *abort_p = 1u;
+    }
+  } else if (lane == 0) {
+    bool ok = true;
+    int xs = 0;
+    uint32_t phase = 1;
+    for (int q = 0; q < n; ++q) {
+      const uint32_t bar = smem_u32(&bars.x_full[xs]), to = base + xs * kBytesX;
+      if (!(ok = mbar_wait(smem_u32(&bars.x_empty[xs]), phase, abort_p))) break;
+      mbar_expect_tx(bar, kBytesX);
+      tma_load_2d(to, &map_x, bar, (first + q) * 128, m0);
+      tma_load_2d(to + kHalfX, &map_x, bar, (first + q) * 128 + 64, m0);
+      if (++xs == kXStages) xs = 0, phase ^= 1u;
+    }
+    if (!ok) {
+      // the copies under way land before the block ends (in their order: the last is the one in front of xs)
+      *abort_p = 1u;
+      uint32_t never = 0;
+      if (phase == 0u || xs > 0)
+        mbar_wait(smem_u32(&bars.x_full[xs == 0 ? kXStages - 1 : xs - 1]), (xs == 0 ? phase : phase ^ 1u), &never, 10000000ll);
+    }
   }
   __syncwarp();
   tc_fence_before();
   __syncthreads();
   if (*abort_p != 0u && threadIdx.x == 0) atomicExch(status, WINO_ERR_TIMEOUT);
-  if (warp == 12) {
+  if (warp == kMmaWarp) {
     tc_fence_after();
     tmem_dealloc(tmem, kColumns);
   }
-  const long out = (long)block_K * 128 + warp * 32 + lane;      // epilogue lanes
-  if (S == 1) {
-    if (warp < 4 && out < a.w.K) {
-      const float bias = a.bias ? a.bias[out] : 0.0f;
-#pragma unroll
-      for (int i = 0; i < NP; ++i)
-        if (m0 + i < a.M) store_output(a.out, (m0 + i) * a.y_row + out, acc[i], bias);
-    }
-    return;
-  }
-  float* sums = reinterpret_cast<float*>(smem_raw);              // [row of x][output]: the rings have been read
+  // Sums by way of shared memory, where the rings were: [row of x][output].  A short loop then finishes them:
+  // laid out in a row, the code for 64 results of any type is 60 KB, and fetching it took 6 us.
+  float* sums = reinterpret_cast<float*>(smem_raw);
   if (warp < 4)
 #pragma unroll
-    for (int i = 0; i < NP; ++i) sums[i * 128 + warp * 32 + lane] = acc[i];
-  cluster.sync();
-  const int rows = min(NP, a.M - m0);
-  for (int e = threadIdx.x + rank * kTcThreads; e < rows * 128; e += kTcThreads * S) {
-    const long k = (long)block_K * 128 + (e & 127);
-    float s = 0.0f;
-    for (int b = 0; b < S; ++b) s = __fadd_rn(s, cluster.map_shared_rank(sums, b)[e]);
-    if (k < a.w.K) store_output(a.out, (m0 + (e >> 7)) * a.y_row + k, s, a.bias ? a.bias[k] : 0.0f);
+    for (int i = 0; i < NP; ++i) {
+      uint32_t v[2];
+      f2_split(acc[i / 2], v[0], v[1]);
+      sums[i * 128 + warp * 32 + lane] = __uint_as_float(v[i & 1]);
+    }
+  if (S > 1) cluster.sync();
+  else __syncthreads();
+  const int rows = min(NP, a.M - m0), k = threadIdx.x & 127, by = kTcThreads / 128 * S;
+  const long out = (long)block_K * 128 + k;
+  if (out < a.w.K && threadIdx.x < kTcThreads / 128 * 128) {
+    const float bias = a.bias ? a.bias[out] : 0.0f;
+#pragma unroll 1
+    for (int m = threadIdx.x / 128 * S + rank; m < rows; m += by) {
+      float s = 0.0f;
+      if (S == 1) {
+        s = sums[m * 128 + k];
+      } else {
+        float v[8];
+#pragma unroll
+        for (int b = 0; b < 8; ++b) v[b] = b < S ? cluster.map_shared_rank(sums, b)[m * 128 + k] : 0.0f;
+#pragma unroll
+        for (int b = 0; b < 8; ++b) s = __fadd_rn(s, v[b]);
+      }
+      store_output(a.out, (m0 + m) * a.y_row + out, s, bias);
+    }
   }
-  cluster.sync();   // no block leaves while another reads its sums
+  if (S > 1) cluster.sync();   // no block leaves while another reads its sums
 }
 
-#ifndef TCBLOCKS
-#define TCBLOCKS 1
-#endif
 template <bool F16, int NP, bool SMALL, bool ZEROS>
 int launch_tc(const LinearArgs& a, int num_sms, int device, int* status, cudaStream_t st) {
   const long blocks = (a.w.K + 127) / 128, slices = (a.M + NP - 1) / NP;
   if (slices > 65535) return WINO_ERR_UNSUPPORTED;
-  const long room = (long)(NP <= 16 ? 2 : 1) * TCBLOCKS * num_sms;
+  // blocks that share the inputs, while there are SMs for them and two chunks for each
   int S = 1;
-  while (S < 8 && blocks * slices * (S + 1) <= room && (S + 1) * 2 <= a.w.tiles_C) ++S;
-  constexpr size_t ring = (size_t)TcShape::kB * NP * 256 + 2 * kTcStages * 8192;
+  while (S < 8 && blocks * slices * (S + 1) <= num_sms && (S + 1) * 2 <= a.w.tiles_C) ++S;
+  constexpr size_t ring = (size_t)kXStages * NP * 256 + kSets * kTcStages * kStageBytes + 4 * kScaleStages * 64;
   constexpr size_t sums = (size_t)NP * 128 * sizeof(float);
   constexpr size_t smem = (ring > sums ? ring : sums) + 1024;
+  CUtensorMap map_x;
+  const uint64_t row = a.M == 1 ? ((uint64_t)a.w.C * 2 + 15) / 16 * 16 : (uint64_t)a.x_row;
+  int rc = encode_rows_16bit(&map_x, a.x, F16, (uint64_t)a.w.C, (uint64_t)a.M, row, 64, NP);
+  if (rc != 0) return rc;
   static DeviceOnce once;
   auto kernel = k_linear_tc<F16, NP, SMALL, ZEROS>;
-  const int rc = set_max_smem(once, device, kernel, smem);
-  if (rc != 0) return rc;
+  if ((rc = set_max_smem(once, device, kernel, smem)) != 0) return rc;
   return launch_kernel_cluster(kernel, dim3((unsigned)(blocks * S), (unsigned)slices), dim3(kTcThreads), (unsigned)S, smem, st,
-                               true, a, status);
+                               true, a, map_x, status);
 }
 template <bool F16, int NP>
 int launch_build(const LinearArgs& a, int num_sms, int device, int* status, cudaStream_t st) {

@@ -222,15 +222,6 @@ __device__ __forceinline__ void to_floats(const Input<DT>& in, float (&v)[8]) {
   }
 }
 
-// The inputs of one tile: x[n][i] of row n at `at[n]` + 32 i, inside the row and aligned.
-template <int DT, int NT>
-__device__ __forceinline__ void load_tile(Input<DT> (&x)[NT][4], const char* const (&at)[NT]) {
-#pragma unroll
-  for (int n = 0; n < NT; ++n)
-#pragma unroll
-    for (int i = 0; i < 4; ++i) x[n][i].load(at[n] + 32 * i * Input<DT>::kBytes);
-}
-
 // Inputs k .. k+7 of the row at `row`, the code of zero beyond C.  vec: rows are aligned to eight elements
 // (at most 16 bytes).
 template <int DT>
@@ -245,6 +236,33 @@ __device__ __forceinline__ Input<DT> load_input(const char* row, int k, int C, b
       if (k + e < C) in.set(e, row + (long)(k + e) * Input<DT>::kBytes);
   }
   return in;
+}
+
+// The inputs of tile c: x[n][i] of the row at row[n], inputs 128 c + 32 i + 8 t on.
+//   VEC  rows are aligned to eight elements and C is a multiple of eight: eight at once, or none
+template <bool VEC, int DT, int NT>
+__device__ __forceinline__ void load_tile(Input<DT> (&x)[NT][4], const char* const (&row)[NT], int c, int C, int z_x, int t) {
+  if (VEC && (c + 1) * 128 <= C) {
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+      const char* at = row[n] + (c * 128l + 8 * t) * Input<DT>::kBytes;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) x[n][i].load(at + 32 * i * Input<DT>::kBytes);
+    }
+    return;
+  }
+#pragma unroll
+  for (int n = 0; n < NT; ++n)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int k = c * 128 + 32 * i + 8 * t;
+      if constexpr (VEC) {
+        x[n][i].clear(z_x);
+        if (k < C) x[n][i].load(row[n] + (long)k * Input<DT>::kBytes);
+      } else {
+        x[n][i] = load_input<DT>(row[n], k, C, false, z_x);
+      }
+    }
 }
 
 // Codes, scales and zeros of one row tile (16 outputs), from its first input on.
