@@ -11,8 +11,8 @@
 //                into the set's buffer of tensor memory; warp w of a set fills lanes 32 (w % 4) .. +31
 //   then a warp that owns the tensor memory and issues the MMAs, and one whose leader copies x by TMA
 //
-// What bounds it is the unpacking (seven instructions of the ALU pipe for eight codes), which is why sixteen
-// of the 22 warps do it, and why x, which needs no conversion, is left to the copy engine.
+// What bounds it is the unpacking (seven instructions of the ALU pipe for eight codes), which is why twelve
+// of the 18 warps do it, and why x, which needs no conversion, is left to the copy engine.
 // Codes are copied in the order they are stored (512 consecutive bytes an instruction) to places in which a
 // lane finds the four units of its own row without bank conflicts: unit t of row r stands at
 // t ^ (r / 2 % 4).  The blocks of a cluster share the inputs and add their sums in a fixed order.
@@ -27,16 +27,8 @@ namespace cg = cooperative_groups;
 
 namespace {
 
-#ifndef SETS
-#define SETS 4
-#endif
-#ifndef CSTAGES
-#define CSTAGES 3
-#endif
-#ifndef XSTAGES
-#define XSTAGES 4
-#endif
-constexpr int kSets = SETS, kTcStages = CSTAGES /* code stages of a set */, kXStages = XSTAGES /* chunks of x */;
+constexpr int kSets = 3, kTcStages = 3 /* code stages of a set */;
+constexpr int kRing = 8;       // chunks of x in shared memory, and of barriers
 constexpr int kMmaWarp = 4 + 4 * kSets, kXWarp = kMmaWarp + 1, kTcThreads = (kXWarp + 1) * 32;
 
 template <bool ACCUMULATE>
@@ -71,30 +63,35 @@ constexpr uint32_t idesc_f16(bool f16, int M, int N) {
   return (1u << 4) | (f16 ? 0u : (1u << 7) | (1u << 10)) | ((uint32_t)(N >> 3) << 17) | ((uint32_t)(M >> 4) << 24);
 }
 
-constexpr int tc_columns(int NP, int slots) {
+// Chunks in tensor memory, operand and sums (of up to four groups: small groups come with NP at most 32).
+constexpr int tc_chunks(int NP, bool small) { return small && NP > 16 ? 2 : 4; }
+constexpr int tc_columns(int NP, bool small) {
   int n = 32;
-  while (n < kSets * 64 + slots * NP) n *= 2;
+  while (n < tc_chunks(NP, small) * (64 + (small ? 4 : 1) * NP)) n *= 2;
   return n;
 }
-constexpr int kSlots = 4;   // of sums
+
+// full: a chunk's operands are there (its four unpacking warps, the copy of x) and the sums it goes to have been
+// read (four epilogue warps); done: its MMAs are over.  One wait and one commit a chunk: the thread that issues
+// them is the only one of its kind, and two more of each a chunk made it the slowest part.
+struct TcBars {
+  uint64_t full[kRing], done[kRing];
+  uint32_t tmem, abort;
+};
 constexpr int kScaleStages = 8;
 // A stage of codes: 128 rows of 64 bytes, and zeros [4 warps][2 row tiles][4 groups][16].
 constexpr uint32_t kZerosAt = 8192, kStageBytes = 8192 + 512;
 
-struct TcBars {
-  uint64_t a_full[kSets], a_empty[kSets], d_full[kSlots], d_empty[kSlots], x_full[kXStages], x_empty[kXStages];
-  uint32_t tmem, abort;
-};
 
 template <bool F16, int NP, bool SMALL, bool ZEROS>
 __global__ void __launch_bounds__(kTcThreads, 1)
 k_linear_tc(const __grid_constant__ LinearArgs a, const __grid_constant__ CUtensorMap map_x, int* __restrict__ status) {
-  constexpr int kColumns = tc_columns(NP, kSlots);
+  constexpr int kChunks = tc_chunks(NP, SMALL), kColumns = tc_columns(NP, SMALL), kSums = SMALL ? 4 : 1;
   constexpr uint32_t kBytesX = NP * 256, kHalfX = NP * 128;      // a chunk of x: two halves of 64 inputs
   extern __shared__ uint8_t smem_raw[];
   __shared__ TcBars bars;
   const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
-  const uint32_t ring_codes = base + kXStages * kBytesX;         // [set][stage]
+  const uint32_t ring_codes = base + kRing * kBytesX;         // [set][stage]
   const uint32_t scales_at = ring_codes + kSets * kTcStages * kStageBytes;   // [warp][stage][2 row tiles][16]
   const cg::cluster_group cluster = cg::this_cluster();
   const int S = (int)cluster.num_blocks(), rank = (int)cluster.block_rank();
@@ -105,17 +102,9 @@ k_linear_tc(const __grid_constant__ LinearArgs a, const __grid_constant__ CUtens
   volatile uint32_t* abort_p = &bars.abort;
 
   if (threadIdx.x == 0) {
-    for (int i = 0; i < kSets; ++i) {
-      mbar_init(smem_u32(&bars.a_full[i]), 4);
-      mbar_init(smem_u32(&bars.a_empty[i]), 1);
-    }
-    for (int i = 0; i < kSlots; ++i) {
-      mbar_init(smem_u32(&bars.d_full[i]), 1);
-      mbar_init(smem_u32(&bars.d_empty[i]), 4);
-    }
-    for (int i = 0; i < kXStages; ++i) {
-      mbar_init(smem_u32(&bars.x_full[i]), 1);
-      mbar_init(smem_u32(&bars.x_empty[i]), 1);
+    for (int i = 0; i < kRing; ++i) {
+      mbar_init(smem_u32(&bars.full[i]), 4 + 1 + 4);
+      mbar_init(smem_u32(&bars.done[i]), 1);
     }
     bars.abort = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -129,7 +118,7 @@ k_linear_tc(const __grid_constant__ LinearArgs a, const __grid_constant__ CUtens
   __syncthreads();
   tc_fence_after();
   griddep_launch();
-  const uint32_t tmem = bars.tmem, tmem_d = tmem + kSets * 64;
+  const uint32_t tmem = bars.tmem, tmem_d = tmem + kChunks * 64;
 
   F2 acc[NP / 2];                                                // epilogue only: rows of x 2 i, 2 i + 1
   if (warp < 4) {
@@ -149,33 +138,38 @@ k_linear_tc(const __grid_constant__ LinearArgs a, const __grid_constant__ CUtens
       }
       asm volatile("cp.async.commit_group;" ::: "memory");
     };
+    if (lane == 0)
+      for (int i = 0; i < kChunks; ++i) mbar_arrive(smem_u32(&bars.full[i]));      // nothing to read yet
     for (int i = 0; i < kScaleStages; ++i) copy(i);
     bool ok = true;
-    int slot = 0;
-    uint32_t phase = 0;
-    for (int i = 0; i < all; ++i) {
-      asm volatile("cp.async.wait_group %0;" ::"n"(kScaleStages - 1) : "memory");
-      __syncwarp();
-      const F2 s = f2_both(scale_to_float((uint16_t)lds_u16(ring + (i % kScaleStages) * 64 + lane * 2), a.w.scale_f16));
-      ok = __all_sync(0xffffffffu, mbar_wait<false>(smem_u32(&bars.d_full[slot]), phase, abort_p));
+    int i = 0;
+    for (int q = 0; q < n; ++q) {
+      ok = __all_sync(0xffffffffu, mbar_wait<false>(smem_u32(&bars.done[q % kRing]), (q / kRing) & 1, abort_p));
       if (!ok) break;
-      copy(i + kScaleStages);            // every lane has read its scale
       tc_fence_after();
-      const uint32_t from = tmem_d + slot * NP + ((uint32_t)(warp * 32) << 16);
+      for (int p = 0; p < parts; ++p, ++i) {
+        asm volatile("cp.async.wait_group %0;" ::"n"(kScaleStages - 1) : "memory");
+        __syncwarp();
+        const F2 s = f2_both(scale_to_float((uint16_t)lds_u16(ring + (i % kScaleStages) * 64 + lane * 2), a.w.scale_f16));
+        const uint32_t from = tmem_d + (q % kChunks * kSums + p) * NP + ((uint32_t)(warp * 32) << 16);
 #pragma unroll
-      for (int col = 0; col < NP; col += 16) {
-        uint32_t d[16];
-        tmem_ld16(from + col, d);
-        tmem_ld_wait();
-        if (col + 16 == NP) {
-          tc_fence_before();
-          __syncwarp();
-          if (lane == 0) mbar_arrive(smem_u32(&bars.d_empty[slot]));
+        for (int col = 0; col < NP; col += 32) {
+          constexpr int kCols = NP < 32 ? NP : 32;
+          uint32_t d[kCols];
+          if constexpr (kCols == 32) tmem_ld32(from + col, d);
+          else tmem_ld16(from + col, d);
+          tmem_ld_wait();
+          if (col + kCols == NP && p + 1 == parts) {
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(smem_u32(&bars.full[(q + kChunks) % kRing]));
+          }
+#pragma unroll
+          for (int e = 0; e < kCols / 2; ++e) acc[col / 2 + e] = v_fma(f2_bits(d[2 * e], d[2 * e + 1]), s, acc[col / 2 + e]);
         }
-#pragma unroll
-        for (int e = 0; e < 8; ++e) acc[col / 2 + e] = v_fma(f2_bits(d[2 * e], d[2 * e + 1]), s, acc[col / 2 + e]);
+        __syncwarp();
+        copy(i + kScaleStages);            // every lane has read its scale
       }
-      if (++slot == kSlots) slot = 0, phase ^= 1u;
     }
     if (!ok) *abort_p = 1u;
     asm volatile("cp.async.wait_all;" ::: "memory");
@@ -210,10 +204,8 @@ k_linear_tc(const __grid_constant__ LinearArgs a, const __grid_constant__ CUtens
     };
     for (int d = 0; d < kTcStages; ++d) copy(d * kStageBytes);
     const uint32_t row_at = codes_at + lane * 64, swap = (uint32_t)(lane >> 1 & 3) << 4;
-    const uint32_t a_at = tmem + set * 64 + ((uint32_t)(quad * 32) << 16);
-    const uint32_t full = smem_u32(&bars.a_full[set]), empty = smem_u32(&bars.a_empty[set]);
     bool ok = true;
-    uint32_t stage = 0, phase = 1;
+    uint32_t stage = 0;
     for (int q = set; q < n; q += kSets) {
       asm volatile("cp.async.wait_group %0;" ::"n"(kTcStages - 1) : "memory");
       __syncwarp();
@@ -235,12 +227,13 @@ k_linear_tc(const __grid_constant__ LinearArgs a, const __grid_constant__ CUtens
             for (int p = 0; p < 4; ++p) r[i * 16 + t * 4 + p] = v[p];
           }
         }
-        if (h == 0) {
-          ok = __all_sync(0xffffffffu, mbar_wait<false>(empty, phase, abort_p));
+        if (h == 0 && q >= kChunks) {        // what was there has been multiplied
+          const int before = q - kChunks;
+          ok = __all_sync(0xffffffffu, mbar_wait<false>(smem_u32(&bars.done[before % kRing]), (before / kRing) & 1, abort_p));
           if (!ok) break;
           tc_fence_after();
         }
-        tmem_st32(a_at + h * 32, r);
+        tmem_st32(tmem + q % kChunks * 64 + h * 32 + ((uint32_t)(quad * 32) << 16), r);
       }
       if (!ok) break;
       __syncwarp();
@@ -248,8 +241,7 @@ k_linear_tc(const __grid_constant__ LinearArgs a, const __grid_constant__ CUtens
       tmem_st_wait();
       tc_fence_before();
       __syncwarp();
-      if (lane == 0) mbar_arrive(full);
-      phase ^= 1u;
+      if (lane == 0) mbar_arrive(smem_u32(&bars.full[q % kRing]));
       stage = stage == (kTcStages - 1) * kStageBytes ? 0 : stage + kStageBytes;
     }
     if (!ok) *abort_p = 1u;
@@ -262,56 +254,41 @@ k_linear_tc(const __grid_constant__ LinearArgs a, const __grid_constant__ CUtens
       const uint64_t desc0 = make_desc_sw128(base);
       const uint32_t desc_hi = (uint32_t)(desc0 >> 32);
       bool ok = true;
-      int slot = 0, set = 0, xs = 0;
-      uint32_t d_phase = 1, a_phase = 0, x_phase = 0;
       for (int q = 0; q < n; ++q) {
-        if (!(ok = mbar_wait<false>(smem_u32(&bars.x_full[xs]), x_phase, abort_p))) break;
-        if (!(ok = mbar_wait<false>(smem_u32(&bars.a_full[set]), a_phase, abort_p))) break;
-        const uint32_t desc = (uint32_t)desc0 + xs * (kBytesX >> 4), from = tmem + set * 64;
+        const int at = q % kRing, to = q % kChunks;
+        if (!(ok = mbar_wait<false>(smem_u32(&bars.full[at]), (q / kRing) & 1, abort_p))) break;
+        tc_fence_after();
+        const uint32_t desc = (uint32_t)desc0 + at * (kBytesX >> 4), from = tmem + to * 64, sum0 = tmem_d + to * kSums * NP;
 #pragma unroll
         for (int k = 0; k < 8; ++k) {                            // inputs 16 k .. +15
-          const bool begins = SMALL ? k % (parts == 4 ? 2 : 4) == 0 : k == 0;
-          const bool ends = SMALL ? k % (parts == 4 ? 2 : 4) == (parts == 4 ? 1 : 3) : k == 7;
-          if (begins) {
-            if (!(ok = mbar_wait<false>(smem_u32(&bars.d_empty[slot]), d_phase, abort_p))) break;
-            tc_fence_after();
-          }
-          const uint32_t d = tmem_d + slot * NP, b = desc + (k >> 2) * (kHalfX >> 4) + (k & 3) * 2;
+          const uint32_t b = desc + (k >> 2) * (kHalfX >> 4) + (k & 3) * 2;
+          const bool begins = SMALL ? (parts == 4 ? k % 2 == 0 : k % 4 == 0) : k == 0;
+          const uint32_t d = sum0 + (SMALL ? (parts == 4 ? k / 2 : k / 4) * NP : 0);
           if (begins) mma_f16_ts<false>(d, from + k * 8, b, desc_hi, idesc);
           else mma_f16_ts<true>(d, from + k * 8, b, desc_hi, idesc);
-          if (ends) {
-            mma_commit(smem_u32(&bars.d_full[slot]));
-            if (++slot == kSlots) slot = 0, d_phase ^= 1u;
-          }
         }
-        if (!ok) break;
-        mma_commit(smem_u32(&bars.a_empty[set]));
-        mma_commit(smem_u32(&bars.x_empty[xs]));
-        if (++set == kSets) set = 0, a_phase ^= 1u;
-        if (++xs == kXStages) xs = 0, x_phase ^= 1u;
+        mma_commit(smem_u32(&bars.done[at]));
       }
-      // the last commit has arrived (commits arrive in order)
-      ok = ok && mbar_wait<false>(smem_u32(&bars.x_empty[(n - 1) % kXStages]), ((n - 1) / kXStages) & 1, abort_p);
+      // the last commit has arrived
+      ok = ok && mbar_wait<false>(smem_u32(&bars.done[(n - 1) % kRing]), ((n - 1) / kRing) & 1, abort_p);
       if (!ok) *abort_p = 1u;
     }
   } else if (lane == 0) {
     bool ok = true;
-    int xs = 0;
-    uint32_t phase = 1;
-    for (int q = 0; q < n; ++q) {
-      const uint32_t bar = smem_u32(&bars.x_full[xs]), to = base + xs * kBytesX;
-      if (!(ok = mbar_wait(smem_u32(&bars.x_empty[xs]), phase, abort_p))) break;
+    int q = 0;
+    for (; q < n; ++q) {
+      const int at = q % kRing;
+      const uint32_t bar = smem_u32(&bars.full[at]), to = base + at * kBytesX;
+      if (q >= kRing && !(ok = mbar_wait(smem_u32(&bars.done[at]), ((q / kRing) & 1) ^ 1, abort_p))) break;
       mbar_expect_tx(bar, kBytesX);
       tma_load_2d(to, &map_x, bar, (first + q) * 128, m0);
       tma_load_2d(to + kHalfX, &map_x, bar, (first + q) * 128 + 64, m0);
-      if (++xs == kXStages) xs = 0, phase ^= 1u;
     }
     if (!ok) {
-      // the copies under way land before the block ends (in their order: the last is the one in front of xs)
+      // A wait elsewhere ran out: the copies under way get time to land before the block ends.
       *abort_p = 1u;
-      uint32_t never = 0;
-      if (phase == 0u || xs > 0)
-        mbar_wait(smem_u32(&bars.x_full[xs == 0 ? kXStages - 1 : xs - 1]), (xs == 0 ? phase : phase ^ 1u), &never, 10000000ll);
+      const long long t0 = clock64();
+      while (clock64() - t0 < 10000000ll) __nanosleep(1000);
     }
   }
   __syncwarp();
@@ -363,7 +340,7 @@ int launch_tc(const LinearArgs& a, int num_sms, int device, int* status, cudaStr
   // blocks that share the inputs, while there are SMs for them and two chunks for each
   int S = 1;
   while (S < 8 && blocks * slices * (S + 1) <= num_sms && (S + 1) * 2 <= a.w.tiles_C) ++S;
-  constexpr size_t ring = (size_t)kXStages * NP * 256 + kSets * kTcStages * kStageBytes + 4 * kScaleStages * 64;
+  constexpr size_t ring = (size_t)kRing * NP * 256 + kSets * kTcStages * kStageBytes + 4 * kScaleStages * 64;
   constexpr size_t sums = (size_t)NP * 128 * sizeof(float);
   constexpr size_t smem = (ring > sums ? ring : sums) + 1024;
   CUtensorMap map_x;
@@ -386,9 +363,11 @@ int launch_build(const LinearArgs& a, int num_sms, int device, int* status, cuda
 }
 template <bool F16>
 int launch_width(const LinearArgs& a, int num_sms, int device, int* status, cudaStream_t st) {
-  return a.M <= 16 ? launch_build<F16, 16>(a, num_sms, device, status, st)
-       : a.M <= 32 ? launch_build<F16, 32>(a, num_sms, device, status, st)
-                   : launch_build<F16, 64>(a, num_sms, device, status, st);
+  if (a.M <= 16) return launch_build<F16, 16>(a, num_sms, device, status, st);
+  if (a.M <= 32 || a.w.group < 128) return launch_build<F16, 32>(a, num_sms, device, status, st);
+  // (64 rows of x and small groups would take more than 512 columns of tensor memory)
+  return a.w.zeros ? launch_tc<F16, 64, false, true>(a, num_sms, device, status, st)
+                   : launch_tc<F16, 64, false, false>(a, num_sms, device, status, st);
 }
 
 }  // namespace

@@ -20,16 +20,23 @@ struct QuantizeArgs {
 
 constexpr int kQuantWarps = 4;
 
-template <int DT>
+// FULL: rows of w and of the values are aligned to eight elements, and C is a multiple of 128
+template <bool FULL, int DT>
 __device__ __forceinline__ void load_weights(const QuantizeArgs& a, const char* row, int k, float (&v)[8]) {
+  if constexpr (FULL) {
+    Input<DT> in;
+    in.load(row + (long)k * Input<DT>::kBytes);
+    to_floats<DT>(in, v);
+    return;
+  }
   to_floats<DT>(load_input<DT>(row, k, a.C, a.vec, 0), v);
 }
 
-template <int DT>
+template <bool FULL, int DT>
 __device__ __forceinline__ void store_values(const QuantizeArgs& a, char* row, int k, const float (&v)[8]) {
   if constexpr (DT == WINO_FLOAT) {
     float* p = reinterpret_cast<float*>(row) + k;
-    if (a.vec_values && k + 8 <= a.C) {
+    if (FULL || (a.vec_values && k + 8 <= a.C)) {
       reinterpret_cast<float4*>(p)[0] = make_float4(v[0], v[1], v[2], v[3]);
       reinterpret_cast<float4*>(p)[1] = make_float4(v[4], v[5], v[6], v[7]);
     } else {
@@ -37,17 +44,23 @@ __device__ __forceinline__ void store_values(const QuantizeArgs& a, char* row, i
       for (int e = 0; e < 8; ++e) if (k + e < a.C) p[e] = v[e];
     }
   } else {
-    uint16_t h[8];
+    uint32_t h[4];
 #pragma unroll
-    for (int e = 0; e < 8; ++e)
-      h[e] = DT == WINO_FP16 ? __half_as_ushort(__float2half_rn(v[e])) : __bfloat16_as_ushort(__float2bfloat16_rn(v[e]));
+    for (int j = 0; j < 4; ++j) {
+      if constexpr (DT == WINO_FP16) {
+        const __half2 p = __floats2half2_rn(v[2 * j], v[2 * j + 1]);
+        h[j] = *reinterpret_cast<const uint32_t*>(&p);
+      } else {
+        const __nv_bfloat162 p = __floats2bfloat162_rn(v[2 * j], v[2 * j + 1]);
+        h[j] = *reinterpret_cast<const uint32_t*>(&p);
+      }
+    }
     uint16_t* p = reinterpret_cast<uint16_t*>(row) + k;
-    if (a.vec_values && k + 8 <= a.C) {
-      *reinterpret_cast<uint4*>(p) = make_uint4(h[0] | (uint32_t)h[1] << 16, h[2] | (uint32_t)h[3] << 16,
-                                                h[4] | (uint32_t)h[5] << 16, h[6] | (uint32_t)h[7] << 16);
+    if (FULL || (a.vec_values && k + 8 <= a.C)) {
+      *reinterpret_cast<uint4*>(p) = make_uint4(h[0], h[1], h[2], h[3]);
     } else {
 #pragma unroll
-      for (int e = 0; e < 8; ++e) if (k + e < a.C) p[e] = h[e];
+      for (int e = 0; e < 8; ++e) if (k + e < a.C) p[e] = (uint16_t)(h[e >> 1] >> (16 * (e & 1)));
     }
   }
 }
@@ -66,7 +79,7 @@ struct Range {
   }
 };
 
-struct Grid { float s, z; uint16_t bits; };
+struct Grid { float s, z, inverse; uint16_t bits; };
 __device__ __forceinline__ Grid grid_of(const QuantizeArgs& a, const Range& r) {
   Grid q;
   const float span = a.zeros ? __fdiv_rn(__fsub_rn(r.hi, r.lo), 15.0f) : __fdiv_rn(fmaxf(r.hi, -r.lo), 7.0f);
@@ -76,28 +89,50 @@ __device__ __forceinline__ Grid grid_of(const QuantizeArgs& a, const Range& r) {
     q.bits = __bfloat16_as_ushort(__float2bfloat16_rn(fminf(span, __uint_as_float(0x7F7F0000u))));
   }
   q.s = scale_to_float(q.bits, a.scale_f16);
+  q.inverse = q.s > 0.0f ? __frcp_rn(q.s) : 0.0f;
   q.z = a.zeros && q.s > 0.0f ? fminf(fmaxf(rintf(__fdiv_rn(-r.lo, q.s)), 0.0f), 15.0f) : 8.0f;
   return q;
 }
 
-template <int DT>
+// w / s in 32 bits for scales far from the ends of the floats' range, as the reciprocal's product and one
+// correction by its exact remainder: with the correctly rounded 1 / s that is the correctly rounded quotient
+// (Markstein, Computation of elementary functions on the IBM RISC System/6000 processor, 1990).  Three
+// instructions, where a division's special cases and their code took 8192 x 8192 bf16 weights from 60 to 115 us.
+__device__ __forceinline__ bool plain_scale(float s) { return s == 0.0f || (s >= 0x1p-100f && s <= 0x1p100f); }
+__device__ __forceinline__ float quotient(float w, const Grid& q) {
+  const float r = __fmul_rn(w, q.inverse);
+  const float rest = fminf(__fmaf_rn(-r, q.s, w), q.s);     // of an infinite r: not a number, and then s
+  return __fmaf_rn(rest, q.inverse, r);
+}
+__device__ __noinline__ float any_quotient(float w, float s) { return __fdiv_rn(w, s); }
+
+template <bool FULL, int DT>
 __device__ __forceinline__ uint32_t codes_of(const QuantizeArgs& a, const Grid& q, const float (&v)[8], char* out, int k) {
   uint32_t word = 0;
-  float back[8];
+  float back[8], r[8];
+  if (plain_scale(q.s)) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) r[e] = quotient(v[e], q);
+  } else {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) r[e] = any_quotient(v[e], q.s);
+  }
+  const float zero = __fadd_rn(kMagic, q.z);
 #pragma unroll
   for (int e = 0; e < 8; ++e) {
-    const float c = q.s > 0.0f ? fminf(fmaxf(__fadd_rn(rintf(__fdiv_rn(v[e], q.s)), q.z), 0.0f), 15.0f) : q.z;
-    back[e] = __fmul_rn(__fsub_rn(c, q.z), q.s);
-    word |= (uint32_t)(int)c << (4 * (e / 2 + 4 * (e & 1)));
+    // kMagic + code, clamped as such: the code is in the low bits, what is above them goes with the sum
+    const float c = fminf(fmaxf(__fadd_rn(__fadd_rn(r[e], kMagic), q.z), kMagic), kMagic + 15.0f);
+    back[e] = __fmul_rn(__fsub_rn(c, zero), q.s);
+    word += (uint32_t)__float_as_int(c) * (1u << (4 * (e / 2 + 4 * (e & 1))));
   }
-  if (out != nullptr) store_values<DT>(a, out, k, back);
-  return word;
+  if (out != nullptr) store_values<FULL, DT>(a, out, k, back);
+  return word - (uint32_t)kMagicBits * 0x11111111u;
 }
 
 // grid.x: warps over (pairs of half tiles of outputs) x parts of the inputs; span: tiles of inputs that a
 // warp takes, whole groups
-template <int DT>
-__global__ void __launch_bounds__(kQuantWarps * 32)
+template <bool FULL, int DT>
+__global__ void __launch_bounds__(kQuantWarps * 32, FULL ? 8 : 1)
 k_quantize(const __grid_constant__ QuantizeArgs a, int span, int parts) {
   const int lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
   const long unit = blockIdx.x * (long)kQuantWarps + (threadIdx.x >> 5);
@@ -126,12 +161,17 @@ k_quantize(const __grid_constant__ QuantizeArgs a, int span, int parts) {
       float v[4][8];
       Range r[4];
 #pragma unroll
-      for (int i = 0; i < 4; ++i) load_weights<DT>(a, row, c * 128 + 32 * i + 8 * t, v[i]);
+      for (int i = 0; i < 4; ++i) load_weights<FULL, DT>(a, row, c * 128 + 32 * i + 8 * t, v[i]);
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         r[i].lo = r[i].hi = 0.0f;
+        if (a.zeros) {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) r[i].join(v[i][e]);
+          for (int e = 0; e < 8; ++e) r[i].join(v[i][e]);
+        } else {
+#pragma unroll
+          for (int e = 0; e < 8; ++e) r[i].hi = fmaxf(r[i].hi, fabsf(v[i][e]));
+        }
       }
       if (per >= 2) { r[0].join(r[1]); r[2].join(r[3]); }
       if (per == 4) r[0].join(r[2]);
@@ -139,13 +179,13 @@ k_quantize(const __grid_constant__ QuantizeArgs a, int span, int parts) {
       Grid q;
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        if (i % per == 0) {
+        if ((i & (per - 1)) == 0) {
           r[i].join_lanes();
           q = grid_of(a, r[i]);
-          put(c * (4 / per) + i / per, q);
+          put(per == 1 ? c * 4 + i : per == 2 ? c * 2 + (i >> 1) : c, q);
         }
-        if (!in) q.s = 0.0f, q.z = 8.0f;
-        word[i] = codes_of<DT>(a, q, v[i], out, c * 128 + 32 * i + 8 * t);
+        if (!in) q.s = q.inverse = 0.0f, q.z = 8.0f;
+        word[i] = codes_of<FULL, DT>(a, q, v[i], out, c * 128 + 32 * i + 8 * t);
       }
       codes[c * 64l] = make_uint4(word[0], word[1], word[2], word[3]);
     }
@@ -160,21 +200,21 @@ k_quantize(const __grid_constant__ QuantizeArgs a, int span, int parts) {
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         float v[8];
-        load_weights<DT>(a, row, c * 128 + 32 * i + 8 * t, v);
+        load_weights<FULL, DT>(a, row, c * 128 + 32 * i + 8 * t, v);
 #pragma unroll
         for (int e = 0; e < 8; ++e) r.join(v[e]);
       }
     r.join_lanes();
     Grid q = grid_of(a, r);
     put(c0 / per, q);
-    if (!in) q.s = 0.0f, q.z = 8.0f;
+    if (!in) q.s = q.inverse = 0.0f, q.z = 8.0f;
     for (int c = c0; c < c1; ++c) {
       uint32_t word[4];
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         float v[8];
-        load_weights<DT>(a, row, c * 128 + 32 * i + 8 * t, v);
-        word[i] = codes_of<DT>(a, q, v, out, c * 128 + 32 * i + 8 * t);
+        load_weights<FULL, DT>(a, row, c * 128 + 32 * i + 8 * t, v);
+        word[i] = codes_of<FULL, DT>(a, q, v, out, c * 128 + 32 * i + 8 * t);
       }
       codes[c * 64l] = make_uint4(word[0], word[1], word[2], word[3]);
     }
@@ -198,8 +238,10 @@ int launch_quantize(const wino_packed_t& o, const void* w, int w_dtype, int64_t 
   const int span = per, parts = (a.tiles_C + span - 1) / span;
   const long blocks = (halves * parts + kQuantWarps - 1) / kQuantWarps;
   if (blocks > 0x7fffffffl) return WINO_ERR_UNSUPPORTED;
-  auto kernel = w_dtype == WINO_FLOAT ? k_quantize<WINO_FLOAT> : w_dtype == WINO_BF16 ? k_quantize<WINO_BF16>
-                                                                                       : k_quantize<WINO_FP16>;
+  const bool full = a.vec && (values == nullptr || a.vec_values) && a.C % 128 == 0;
+  auto kernel = w_dtype == WINO_FLOAT  ? (full ? k_quantize<true, WINO_FLOAT> : k_quantize<false, WINO_FLOAT>)
+                : w_dtype == WINO_BF16 ? (full ? k_quantize<true, WINO_BF16> : k_quantize<false, WINO_BF16>)
+                                       : (full ? k_quantize<true, WINO_FP16> : k_quantize<false, WINO_FP16>);
   return launch_kernel(kernel, dim3((unsigned)blocks), dim3(kQuantWarps * 32), 0, st, true, a, span, parts);
 }
 
