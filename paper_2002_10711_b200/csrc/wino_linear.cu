@@ -159,7 +159,7 @@ int launch_type(const LinearArgs& a, int num_sms, cudaStream_t st) {
 
 }  // namespace
 #ifndef TCMIN
-#define TCMIN 17
+#define TCMIN 9
 #endif
 int launch_linear(const wino_linear_desc_t& d, const void* x, const float* bias, void* y, int num_sms,
                   cudaStream_t st) {

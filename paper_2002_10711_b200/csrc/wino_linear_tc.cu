@@ -6,13 +6,15 @@
 // A group's products are accumulated on their own, in a slot of NP columns of tensor memory, and leave it
 // multiplied by the output's scale into 32-bit sums in registers: no weight is rounded.
 //
-//   warps 0-3    epilogue: lane = output; slot -> registers, times the scale, added up
+//   warps 0-7    epilogue: lane = output; sums of a chunk -> registers, times the scale, added up.  Two sets of four
+//                take chunks in turn, or, for 64 rows of x, half of the rows each: one set alone took 500 to
+//                900 cycles a chunk, longer than everything else
 //   then kSets sets of four warps that take chunks in turn: copies of codes several chunks ahead, unpacking
 //                into the set's buffer of tensor memory; warp w of a set fills lanes 32 (w % 4) .. +31
 //   then a warp that owns the tensor memory and issues the MMAs, and one whose leader copies x by TMA
 //
 // What bounds it is the unpacking (seven instructions of the ALU pipe for eight codes), which is why twelve
-// of the 18 warps do it, and why x, which needs no conversion, is left to the copy engine.
+// of the 22 warps do it, and why x, which needs no conversion, is left to the copy engine.
 // Codes are copied in the order they are stored (512 consecutive bytes an instruction) to places in which a
 // lane finds the four units of its own row without bank conflicts: unit t of row r stands at
 // t ^ (r / 2 % 4).  The blocks of a cluster share the inputs and add their sums in a fixed order.
@@ -29,7 +31,7 @@ namespace {
 
 constexpr int kSets = 3, kTcStages = 3 /* code stages of a set */;
 constexpr int kRing = 8;       // chunks of x in shared memory, and of barriers
-constexpr int kMmaWarp = 4 + 4 * kSets, kXWarp = kMmaWarp + 1, kTcThreads = (kXWarp + 1) * 32;
+constexpr int kEpiWarps = 8, kMmaWarp = kEpiWarps + 4 * kSets, kXWarp = kMmaWarp + 1, kTcThreads = (kXWarp + 1) * 32;
 
 template <bool ACCUMULATE>
 __device__ __forceinline__ void mma_f16_ts(uint32_t d, uint32_t a, uint32_t bdesc_lo, uint32_t bdesc_hi, uint32_t idesc) {
@@ -72,7 +74,7 @@ constexpr int tc_columns(int NP, bool small) {
 }
 
 // full: a chunk's operands are there (its four unpacking warps, the copy of x) and the sums it goes to have been
-// read (four epilogue warps); done: its MMAs are over.  One wait and one commit a chunk: the thread that issues
+// read (the epilogue's warps); done: its MMAs are over.  One wait and one commit a chunk: the thread that issues
 // them is the only one of its kind, and two more of each a chunk made it the slowest part.
 struct TcBars {
   uint64_t full[kRing], done[kRing];
@@ -87,6 +89,8 @@ template <bool F16, int NP, bool SMALL, bool ZEROS>
 __global__ void __launch_bounds__(kTcThreads, 1)
 k_linear_tc(const __grid_constant__ LinearArgs a, const __grid_constant__ CUtensorMap map_x, int* __restrict__ status) {
   constexpr int kChunks = tc_chunks(NP, SMALL), kColumns = tc_columns(NP, SMALL), kSums = SMALL ? 4 : 1;
+  constexpr bool kAlternate = NP <= 32;                          // the epilogue's sets take chunks in turn
+  constexpr int kRows = kAlternate ? NP : NP / 2;                // of x, of an epilogue warp
   constexpr uint32_t kBytesX = NP * 256, kHalfX = NP * 128;      // a chunk of x: two halves of 64 inputs
   extern __shared__ uint8_t smem_raw[];
   __shared__ TcBars bars;
@@ -103,7 +107,7 @@ k_linear_tc(const __grid_constant__ LinearArgs a, const __grid_constant__ CUtens
 
   if (threadIdx.x == 0) {
     for (int i = 0; i < kRing; ++i) {
-      mbar_init(smem_u32(&bars.full[i]), 4 + 1 + 4);
+      mbar_init(smem_u32(&bars.full[i]), 4 + 1 + (kAlternate ? 4 : 8));
       mbar_init(smem_u32(&bars.done[i]), 1);
     }
     bars.abort = 0;
@@ -120,61 +124,61 @@ k_linear_tc(const __grid_constant__ LinearArgs a, const __grid_constant__ CUtens
   griddep_launch();
   const uint32_t tmem = bars.tmem, tmem_d = tmem + kChunks * 64;
 
-  F2 acc[NP / 2];                                                // epilogue only: rows of x 2 i, 2 i + 1
-  if (warp < 4) {
+  F2 acc[kRows / 2];                                             // epilogue only: rows of x 2 i, 2 i + 1
 #pragma unroll
-    for (int i = 0; i < NP / 2; ++i) acc[i] = f2_both(0.0f);
-    // Scales of the warp's two row tiles, 64 bytes a sum, copied kScaleStages sums ahead by lanes 0 .. 3.  (Held in
+  for (int i = 0; i < kRows / 2; ++i) acc[i] = f2_both(0.0f);
+  const int quad = warp & 3, epi = warp >> 2;
+  if (warp < kEpiWarps) {
+    // Scales of the warp's two row tiles, 64 bytes a sum, copied some sums ahead by lanes 0 .. 3.  (Held in
     // registers they would be waited for wherever a register is moved.)
-    const long row_tile = min(block_K * 8 + warp * 2 + (lane >> 1 & 1), tiles_K - 1);
+    constexpr int kStep = kAlternate ? 2 : 1;                    // chunks
+    const long row_tile = min(block_K * 8 + quad * 2 + (lane >> 1 & 1), tiles_K - 1);
+    const int q0 = kAlternate ? epi : 0, per = SMALL ? 1 : a.w.group >> 7;
     const char* from_scales = reinterpret_cast<const char*>(a.w.scales + row_tile * a.w.groups * 16) + (lane & 1) * 16;
     const uint32_t ring = scales_at + warp * kScaleStages * 64;
-    const int per = SMALL ? 1 : a.w.group >> 7, all = n * parts;
-    auto copy = [&](int i) {
-      if (i < all && lane < 4) {
-        const int grp = SMALL ? first * parts + i : per == 1 ? first + i : (first + i) / per;
-        asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(ring + (i % kScaleStages) * 64 + lane * 16),
-                     "l"(from_scales + min(grp, a.w.groups - 1) * 32l) : "memory");
+    int next_q = q0, next_p = 0;
+    uint32_t to = 0;
+    auto copy = [&]() {
+      if (lane < 4 && next_q < n) {
+        // (groups behind the last have no inputs: any scale does)
+        const int grp = min(SMALL ? (first + next_q) * parts + next_p : per == 1 ? first + next_q : (first + next_q) / per, a.w.groups - 1);
+        asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(ring + to + lane * 16), "l"(from_scales + grp * 32l) : "memory");
       }
       asm volatile("cp.async.commit_group;" ::: "memory");
+      if (!SMALL || ++next_p == parts) next_p = 0, next_q += kStep;
+      to = (to + 64) % (kScaleStages * 64);
     };
     if (lane == 0)
-      for (int i = 0; i < kChunks; ++i) mbar_arrive(smem_u32(&bars.full[i]));      // nothing to read yet
-    for (int i = 0; i < kScaleStages; ++i) copy(i);
+      for (int i = q0; i < kChunks; i += kStep) mbar_arrive(smem_u32(&bars.full[i]));      // nothing to read yet
+    for (int i = 0; i < kScaleStages; ++i) copy();
     bool ok = true;
-    int i = 0;
-    for (int q = 0; q < n; ++q) {
+    uint32_t at = 0;
+    for (int q = q0; q < n; q += kStep) {
       ok = __all_sync(0xffffffffu, mbar_wait<false>(smem_u32(&bars.done[q % kRing]), (q / kRing) & 1, abort_p));
       if (!ok) break;
       tc_fence_after();
-      for (int p = 0; p < parts; ++p, ++i) {
+      for (int p = 0; p < parts; ++p) {
+        const uint32_t from = tmem_d + (q % kChunks * kSums + p) * NP + (kAlternate ? 0 : epi * kRows) + ((uint32_t)(quad * 32) << 16);
+        uint32_t d[kRows];
+        if constexpr (kRows == 32) tmem_ld32(from, d);
+        else tmem_ld16(from, d);
         asm volatile("cp.async.wait_group %0;" ::"n"(kScaleStages - 1) : "memory");
         __syncwarp();
-        const F2 s = f2_both(scale_to_float((uint16_t)lds_u16(ring + (i % kScaleStages) * 64 + lane * 2), a.w.scale_f16));
-        const uint32_t from = tmem_d + (q % kChunks * kSums + p) * NP + ((uint32_t)(warp * 32) << 16);
+        const F2 s = f2_both(scale_to_float((uint16_t)lds_u16(ring + at + lane * 2), a.w.scale_f16));
+        at = (at + 64) % (kScaleStages * 64);
+        tmem_ld_wait();
+        if (p + 1 == parts) tc_fence_before();
+        __syncwarp();                      // every lane has its scale, and its sums
+        if (p + 1 == parts && lane == 0) mbar_arrive(smem_u32(&bars.full[(q + kChunks) % kRing]));
+        copy();
 #pragma unroll
-        for (int col = 0; col < NP; col += 32) {
-          constexpr int kCols = NP < 32 ? NP : 32;
-          uint32_t d[kCols];
-          if constexpr (kCols == 32) tmem_ld32(from + col, d);
-          else tmem_ld16(from + col, d);
-          tmem_ld_wait();
-          if (col + kCols == NP && p + 1 == parts) {
-            tc_fence_before();
-            __syncwarp();
-            if (lane == 0) mbar_arrive(smem_u32(&bars.full[(q + kChunks) % kRing]));
-          }
-#pragma unroll
-          for (int e = 0; e < kCols / 2; ++e) acc[col / 2 + e] = v_fma(f2_bits(d[2 * e], d[2 * e + 1]), s, acc[col / 2 + e]);
-        }
-        __syncwarp();
-        copy(i + kScaleStages);            // every lane has read its scale
+        for (int e = 0; e < kRows / 2; ++e) acc[e] = v_fma(f2_bits(d[2 * e], d[2 * e + 1]), s, acc[e]);
       }
     }
     if (!ok) *abort_p = 1u;
     asm volatile("cp.async.wait_all;" ::: "memory");
   } else if (warp < kMmaWarp) {
-    const int set = (warp - 4) >> 2, quad = warp & 3;
+    const int set = (warp - kEpiWarps) >> 2;
     const uint32_t ring = ring_codes + set * kTcStages * kStageBytes, codes_at = ring + quad * 2048, zeros_at = ring + kZerosAt + quad * 128;
     // copies: instruction k takes rows 8 k .. 8 k + 7 of the warp's 32
     const uint32_t to = (uint32_t)((lane >> 2) * 64 + (((lane & 3) ^ (lane >> 3 & 3)) << 4));
@@ -302,13 +306,20 @@ k_linear_tc(const __grid_constant__ LinearArgs a, const __grid_constant__ CUtens
   // Sums by way of shared memory, where the rings were: [row of x][output].  A short loop then finishes them:
   // laid out in a row, the code for 64 results of any type is 60 KB, and fetching it took 6 us.
   float* sums = reinterpret_cast<float*>(smem_raw);
-  if (warp < 4)
+  auto put = [&](bool add) {
 #pragma unroll
-    for (int i = 0; i < NP; ++i) {
+    for (int i = 0; i < kRows; ++i) {
       uint32_t v[2];
       f2_split(acc[i / 2], v[0], v[1]);
-      sums[i * 128 + warp * 32 + lane] = __uint_as_float(v[i & 1]);
+      float* to = sums + ((kAlternate ? 0 : epi * kRows) + i) * 128 + quad * 32 + lane;
+      *to = add ? __fadd_rn(*to, __uint_as_float(v[i & 1])) : __uint_as_float(v[i & 1]);
     }
+  };
+  if (warp < 4 || (!kAlternate && warp < kEpiWarps)) put(false);
+  if (kAlternate) {
+    __syncthreads();
+    if (warp >= 4 && warp < kEpiWarps) put(true);
+  }
   if (S > 1) cluster.sync();
   else __syncthreads();
   const int rows = min(NP, a.M - m0), k = threadIdx.x & 127, by = kTcThreads / 128 * S;
@@ -340,7 +351,7 @@ int launch_tc(const LinearArgs& a, int num_sms, int device, int* status, cudaStr
   // blocks that share the inputs, while there are SMs for them and two chunks for each
   int S = 1;
   while (S < 8 && blocks * slices * (S + 1) <= num_sms && (S + 1) * 2 <= a.w.tiles_C) ++S;
-  constexpr size_t ring = (size_t)kRing * NP * 256 + kSets * kTcStages * kStageBytes + 4 * kScaleStages * 64;
+  constexpr size_t ring = (size_t)kRing * NP * 256 + kSets * kTcStages * kStageBytes + kEpiWarps * kScaleStages * 64;
   constexpr size_t sums = (size_t)NP * 128 * sizeof(float);
   constexpr size_t smem = (ring > sums ? ring : sums) + 1024;
   CUtensorMap map_x;
