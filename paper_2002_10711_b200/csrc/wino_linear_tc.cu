@@ -29,9 +29,13 @@ namespace cg = cooperative_groups;
 
 namespace {
 
-constexpr int kSets = 3, kTcStages = 3 /* code stages of a set */;
+// Unpacking sets: three; two beside more than 16 rows of x, where the epilogue wants more registers than 22 warps leave it
+// (what it spilled missed the small L1 cache: 24.7 against 21.4 us for 64 x 8192 x 8192).
+constexpr int tc_sets(int NP) { return NP > 16 ? 2 : 3; }
+constexpr int kTcStages = 3 /* code stages of a set */;
 constexpr int kRing = 8;       // chunks of x in shared memory, and of barriers
-constexpr int kEpiWarps = 8, kMmaWarp = kEpiWarps + 4 * kSets, kXWarp = kMmaWarp + 1, kTcThreads = (kXWarp + 1) * 32;
+constexpr int kEpiWarps = 8;
+constexpr int tc_threads(int NP) { return (kEpiWarps + 4 * tc_sets(NP) + 2) * 32; }
 
 template <bool ACCUMULATE>
 __device__ __forceinline__ void mma_f16_ts(uint32_t d, uint32_t a, uint32_t bdesc_lo, uint32_t bdesc_hi, uint32_t idesc) {
@@ -86,9 +90,10 @@ constexpr uint32_t kZerosAt = 8192, kStageBytes = 8192 + 512;
 
 
 template <bool F16, int NP, bool SMALL, bool ZEROS>
-__global__ void __launch_bounds__(kTcThreads, 1)
+__global__ void __launch_bounds__(tc_threads(NP), 1)
 k_linear_tc(const __grid_constant__ LinearArgs a, const __grid_constant__ CUtensorMap map_x, int* __restrict__ status) {
   constexpr int kChunks = tc_chunks(NP, SMALL), kColumns = tc_columns(NP, SMALL), kSums = SMALL ? 4 : 1;
+  constexpr int kSets = tc_sets(NP), kMmaWarp = kEpiWarps + 4 * kSets, kTcThreads = tc_threads(NP);
   constexpr bool kAlternate = NP <= 32;                          // the epilogue's sets take chunks in turn
   constexpr int kRows = kAlternate ? NP : NP / 2;                // of x, of an epilogue warp
   constexpr uint32_t kBytesX = NP * 256, kHalfX = NP * 128;      // a chunk of x: two halves of 64 inputs
@@ -233,7 +238,7 @@ k_linear_tc(const __grid_constant__ LinearArgs a, const __grid_constant__ CUtens
         }
         if (h == 0 && q >= kChunks) {        // what was there has been multiplied
           const int before = q - kChunks;
-          ok = __all_sync(0xffffffffu, mbar_wait<false>(smem_u32(&bars.done[before % kRing]), (before / kRing) & 1, abort_p));
+          ok = __all_sync(0xffffffffu, mbar_wait<true>(smem_u32(&bars.done[before % kRing]), (before / kRing) & 1, abort_p));
           if (!ok) break;
           tc_fence_after();
         }
@@ -351,7 +356,7 @@ int launch_tc(const LinearArgs& a, int num_sms, int device, int* status, cudaStr
   // blocks that share the inputs, while there are SMs for them and two chunks for each
   int S = 1;
   while (S < 8 && blocks * slices * (S + 1) <= num_sms && (S + 1) * 2 <= a.w.tiles_C) ++S;
-  constexpr size_t ring = (size_t)kRing * NP * 256 + kSets * kTcStages * kStageBytes + kEpiWarps * kScaleStages * 64;
+  constexpr size_t ring = (size_t)kRing * NP * 256 + tc_sets(NP) * kTcStages * kStageBytes + kEpiWarps * kScaleStages * 64;
   constexpr size_t sums = (size_t)NP * 128 * sizeof(float);
   constexpr size_t smem = (ring > sums ? ring : sums) + 1024;
   CUtensorMap map_x;
@@ -361,7 +366,7 @@ int launch_tc(const LinearArgs& a, int num_sms, int device, int* status, cudaStr
   static DeviceOnce once;
   auto kernel = k_linear_tc<F16, NP, SMALL, ZEROS>;
   if ((rc = set_max_smem(once, device, kernel, smem)) != 0) return rc;
-  return launch_kernel_cluster(kernel, dim3((unsigned)(blocks * S), (unsigned)slices), dim3(kTcThreads), (unsigned)S, smem, st,
+  return launch_kernel_cluster(kernel, dim3((unsigned)(blocks * S), (unsigned)slices), dim3(tc_threads(NP)), (unsigned)S, smem, st,
                                true, a, map_x, status);
 }
 template <bool F16, int NP>
