@@ -63,11 +63,14 @@ k_experts_route(const __grid_constant__ ExpertsArgs a) {
   const int S = (int)cluster.num_blocks(), rank = (int)cluster.block_rank();
   const int token = blockIdx.x / S, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   griddep_launch();
-  for (int e = threadIdx.x; e < kMaxExperts; e += kRouteThreads) logits[e] = -INFINITY;   // behind the last: for four at a time
-  cluster.sync();
+  // (behind the last expert: for four at a time)
+  if (rank == 0)
+    for (int e = a.E + threadIdx.x; e < (a.E + 3) / 4 * 4; e += kRouteThreads) logits[e] = -INFINITY;
+  auto arrived = cluster.barrier_arrive();         // the first block is there to be written to: waited for below
   griddep_wait();
   const char* x = a.x + token * a.x_row;
   float* to = cluster.map_shared_rank(logits, 0);
+  bool waits = true;
   for (int e = rank + S * warp; e < a.E; e += S * (kRouteThreads / 32)) {
     const char* r = a.router + (long)e * a.D * In::kBytes;
     float s = 0.0f;
@@ -80,6 +83,7 @@ k_experts_route(const __grid_constant__ ExpertsArgs a) {
     };
     int k = lane * 8;
     if (a.vec && a.vec_router)
+#pragma unroll 1
       for (; k + 3 * 256 + 8 <= a.D; k += 4 * 256) {
         In xi[4], ri[4];
 #pragma unroll
@@ -90,11 +94,14 @@ k_experts_route(const __grid_constant__ ExpertsArgs a) {
 #pragma unroll
         for (int i = 0; i < 4; ++i) add(xi[i], ri[i]);
       }
+#pragma unroll 1
     for (; k < a.D; k += 256) add(load_input<DT>(x, k, a.D, a.vec, 0), load_input<DT>(r, k, a.D, a.vec_router, 0));
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) s = __fadd_rn(s, __shfl_xor_sync(0xffffffffu, s, o));
+    if (waits) cluster.barrier_wait(std::move(arrived)), waits = false;
     if (lane == 0) to[e] = a.router_bias ? __fadd_rn(s, a.router_bias[e]) : s;
   }
+  if (waits) cluster.barrier_wait(std::move(arrived));
   cluster.sync();
   if (rank != 0) return;
   bool odd = false;                       // NaN or +inf
@@ -157,12 +164,27 @@ struct Lists {
 // All threads of the block.
 __device__ __forceinline__ void build_lists(Lists& l, const ExpertsArgs& a) {
   const int pairs = a.T * a.top_k;
+  if (a.T == 1) {
+    // the token's choices as they stand, those of weight 0 last
+    if (threadIdx.x < 32) {
+      const int lane = threadIdx.x;
+      const float w = lane < pairs ? a.weights[lane] : 0.0f;
+      const int e = lane < pairs ? a.ids[lane] : 0;
+      const int chosen = __popc(__ballot_sync(0xffffffffu, w != 0.0f));
+      if (lane <= chosen) l.first[lane] = (uint16_t)lane;
+      if (lane < chosen) l.expert[lane] = (uint16_t)e, l.token[lane] = 0, l.weight[lane] = w;
+      if (lane == 0) l.chosen = chosen;
+    }
+    __syncthreads();
+    return;
+  }
   if (pairs <= 32) {
     // a pair per lane of the first warp: the same experts find one another without a table
     const int lane = threadIdx.x & 31;
     if (threadIdx.x < 32) {
       const float w = lane < pairs ? a.weights[lane] : 0.0f;
-      const int e = lane < pairs && w != 0.0f ? a.ids[lane] : kMaxExperts + lane;
+      const int id = lane < pairs ? a.ids[lane] : 0;
+      const int e = w != 0.0f ? id : kMaxExperts + lane;
       const unsigned same = __match_any_sync(0xffffffffu, e), below = (1u << lane) - 1;
       const bool on = e < kMaxExperts, leads = on && (same & below) == 0;
       // places by expert: how many leaders have smaller ones, and how many pairs
