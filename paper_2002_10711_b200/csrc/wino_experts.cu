@@ -247,13 +247,7 @@ __device__ __forceinline__ void build_lists(Lists& l, const ExpertsArgs& a) {
 }
 
 // ---- gate and up --------------------------------------------------------------------------
-#ifndef UPRING
-#define UPRING 3
-#endif
-#ifndef DOWNRING
-#define DOWNRING 6
-#endif
-constexpr int kUpDepth = UPRING, kDownDepth = DOWNRING;
+constexpr int kUpDepth = 3, kDownDepth = 3, kDownCluster = 8;
 
 // An item is an expert, 8 / split row tiles, and 8 NT of the expert's tokens; a block takes every
 // gridDim.x-th, and has the next one's first tiles on the way while it finishes one.
@@ -359,33 +353,38 @@ k_experts_up(const __grid_constant__ ExpertsArgs a, int split) {
 }
 
 // ---- down -----------------------------------------------------------------------------------
+// A warp takes two row tiles.  The planes of h stand in columns of their own: with two, the eight columns of an
+// MMA are four tokens' upper parts and their lower ones, added up at the end.
 template <int P, int NT, bool SMALL, bool ZEROS>
 __global__ void __launch_bounds__(kExpertWarps * 32)
 k_experts_down(const __grid_constant__ ExpertsArgs a, int split) {
-  using Tiles = Ring<1, 1, SMALL, ZEROS>;
+  using In = Input<WINO_BF16>;
+  using Tiles = Ring<2, 1, SMALL, ZEROS>;
+  constexpr int kEach = P == 2 ? 4 : 2, kTokens = NT * kEach;      // tokens of an MMA's columns, and at a time
   __shared__ Lists lists;
   extern __shared__ __align__(128) uint8_t smem[];
-  float* sums = reinterpret_cast<float*>(smem + kExpertWarps * kDownDepth * Tiles::kSlot);   // [warp][T][17], then [T][17]
+  float* sums = reinterpret_cast<float*>(smem + kExpertWarps * kDownDepth * Tiles::kSlot);   // [warp][T][33]
   const cg::cluster_group cluster = cg::this_cluster();
   const int S = (int)cluster.num_blocks(), rank = (int)cluster.block_rank();
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
   griddep_launch();
-  for (int e = threadIdx.x; e < kExpertWarps * a.T * 17; e += blockDim.x) sums[e] = 0.0f;
+  for (int e = threadIdx.x; e < kExpertWarps * a.T * 33; e += blockDim.x) sums[e] = 0.0f;
   griddep_wait();
   build_lists(lists, a);
-  float* mine = sums + warp * a.T * 17;
+  float* mine = sums + warp * a.T * 33;
   const int per_block = kExpertWarps / split, tiles_K = (a.D + 15) / 16, tiles = a.down.tiles_C;
-  const int tile_K = (int)(blockIdx.x / S) * per_block + warp / split;
+  const int unit = (int)(blockIdx.x / S) * per_block + warp / split;            // two row tiles
   // this warp's part of the tiles of all chosen experts, [expert][tile of inputs]
   const int part = rank * split + warp % split, shared_by = split * S;
   const int all = lists.chosen * tiles;
-  const int u0 = (int)((long)all * part / shared_by), u1 = tile_K < tiles_K ? (int)((long)all * (part + 1) / shared_by) : u0;
+  const int u0 = (int)((long)all * part / shared_by), u1 = unit * 2 < tiles_K ? (int)((long)all * (part + 1) / shared_by) : u0;
   const uint32_t ring = smem_u32(smem) + warp * kDownDepth * Tiles::kSlot, ring_end = ring + kDownDepth * Tiles::kSlot;
   int slot = 0, c = 0, fill_slot = 0, fill_c = 0;
   Tiles from;
   auto start = [&](int s, int at) {
-    const Stream w[1] = {stream_of(expert_of(a.down, lists.expert[s], a.down_units, a.down_scales), tile_K)};
-    from.start(w, a.down, at, tiles, lane);
+    const Packed w = expert_of(a.down, lists.expert[s], a.down_units, a.down_scales);
+    const Stream of[2] = {stream_of(w, unit * 2), stream_of(w, min(unit * 2 + 1, tiles_K - 1))};
+    from.start(of, a.down, at, tiles, lane);
   };
   if (u0 < u1) {
     slot = fill_slot = u0 / tiles;
@@ -399,103 +398,107 @@ k_experts_down(const __grid_constant__ ExpertsArgs a, int split) {
       if (++fill_slot < lists.chosen) start(fill_slot, 0);
     }
   };
-#pragma unroll
+#pragma unroll 1
   for (int d = 0; d < kDownDepth; ++d) {
     if (u0 + d < u1) fill(ring + d * Tiles::kSlot);
     Tiles::commit();
   }
-  float acc[NT][4];
+  float acc[2][NT][4];
 #pragma unroll
-  for (int n = 0; n < NT; ++n) acc[n][0] = acc[n][1] = acc[n][2] = acc[n][3] = 0.0f;
+  for (int n = 0; n < NT; ++n)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) acc[0][n][e] = acc[1][n][e] = 0.0f;
   uint32_t at = ring;
   int first = 0, count = 0;
-  const uint16_t* row[NT];                          // of h, of the first tokens
-  auto row_of = [&](int n) { return a.h + (first + min(n + g, count - 1)) * a.h_row + 8 * t; };
-  auto enter = [&]() {
+  const char* row[NT];                              // of h: this column's plane and token, of the first ones
+  auto enter = [&](int n0) {
+#pragma unroll
+    for (int n = 0; n < NT; ++n)
+      row[n] = reinterpret_cast<const char*>(a.h + min(g / kEach, P - 1) * a.h_plane +
+                                             (first + min(n0 + n * kEach + g % kEach, count - 1)) * a.h_row);
+  };
+  auto expert = [&]() {
     first = lists.first[slot]; count = lists.first[slot + 1] - first;
-#pragma unroll
-    for (int n = 0; n < NT; ++n) row[n] = row_of(8 * n);
+    enter(0);
   };
-  auto load = [&](Planes<P> (&x)[4], const uint16_t* from_h) {
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-#pragma unroll
-      for (int p = 0; p < P; ++p)
-        x[i].v[p] = c * 128 + 32 * i + 8 * t < a.I ? *reinterpret_cast<const uint4*>(from_h + p * a.h_plane + c * 128 + 32 * i)
-                                                   : make_uint4(0, 0, 0, 0);
-  };
-  if (u0 < u1) enter();
-  for (int u = u0; u < u1; ++u) {
-    Planes<P> x[NT][4];
-#pragma unroll
-    for (int n = 0; n < NT; ++n) load(x[n], row[n]);
+  auto multiply = [&]() {
+    In x[NT][4];
+    load_tile<true, WINO_BF16, NT>(x, row, c, a.I, 0, t);       // (rows of h are filled up to eight values)
     Tiles::template wait<kDownDepth - 1>();
-    tile_mma<SMALL, ZEROS, Tiles, NT>(acc, at, 0, a.down, x, 0, lane);
-    const bool last = c + 1 == tiles || u + 1 == u1, more = count > NT * 8;
-    // tokens of the expert, 8 NT at a time; up to that many, sums stay in registers over its tiles
-    if (last || more) {
-      for (int n0 = 0;;) {
+    tile_mma<SMALL, ZEROS, Tiles, NT>(acc[0], at, 0, a.down, x, 0, lane);
+    tile_mma<SMALL, ZEROS, Tiles, NT>(acc[1], at, 1, a.down, x, 0, lane);
+  };
+  if (u0 < u1) expert();
+  for (int u = u0; u < u1; ++u) {
+    // up to kTokens tokens, sums stay in registers over an expert's tiles
+    const bool last = c + 1 == tiles || u + 1 == u1, more = count > kTokens;
+    for (int n0 = 0;;) {
+      multiply();
+      if (last || more) {
 #pragma unroll
-        for (int n = 0; n < NT; ++n)
+        for (int r = 0; r < 2; ++r)
 #pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const int m = n0 + 8 * n + 2 * t + (e & 1);
-            if (m < count) {
-              float* s = mine + lists.token[first + m] * 17 + g + 8 * (e >> 1);
-              *s = __fadd_rn(*s, acc[n][e]);
+          for (int n = 0; n < NT; ++n)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              float v = acc[r][n][e];
+              if (P == 3) v = t == 3 ? 0.0f : __fadd_rn(v, 0.0f);
+              if (P == 3) v = __fadd_rn(v, __shfl_xor_sync(0xffffffffu, v, 1));
+              v = __fadd_rn(v, __shfl_xor_sync(0xffffffffu, v, 2));
+              const int m = n0 + n * kEach + (P == 2 ? 2 * t : 0) + (e & 1);
+              if ((P == 2 ? t < 2 : t == 0) && m < count) {
+                float* s = mine + lists.token[first + m] * 33 + r * 16 + g + 8 * (e >> 1);
+                *s = __fadd_rn(*s, v);
+              }
+              acc[r][n][e] = 0.0f;
             }
-            acc[n][e] = 0.0f;
-          }
-        if ((n0 += NT * 8) >= count) break;
-#pragma unroll
-        for (int n = 0; n < NT; ++n) load(x[n], row_of(n0 + 8 * n));
-        tile_mma<SMALL, ZEROS, Tiles, NT>(acc, at, 0, a.down, x, 0, lane);
       }
+      if (!more || (n0 += kTokens) >= count) break;
+      enter(n0);
     }
+    if (more) enter(0);
     __syncwarp();              // the slot has been read, and `mine` is everyone's
     if (u + kDownDepth < u1) fill(at);
     Tiles::commit();
     if (++c == tiles) {
       c = 0;
       ++slot;
-      if (u + 1 < u1) enter();
+      if (u + 1 < u1) expert();
     }
     at = at + Tiles::kSlot == ring_end ? ring : at + Tiles::kSlot;
   }
   __syncthreads();
-  // outputs of the block: [row tile][token][16], summed over the warps that share the row tile; a cluster's
-  // blocks leave their sums where their first warp's were
-  const int outputs = per_block * a.T * 16;
-  auto finish = [&](int v, int m, int k, float s) {
-    const long out = ((long)(blockIdx.x / S) * per_block + v) * 16 + k;
+  // Outputs of the block, 32 of a token and unit at a time, lane = output, summed over the warps that share the
+  // unit; a cluster's blocks leave their sums where their first warp's were.
+  const int pairs = per_block * a.T;
+  auto finish = [&](int v, int m, float s) {
+    const long out = ((long)(blockIdx.x / S) * per_block + v) * 32 + lane;
     if (out < a.D) store_output(a.out, m * a.y_row + out, s, 0.0f);
   };
-  for (int e = threadIdx.x; e < outputs; e += kExpertWarps * 32) {
-    const int k = e & 15, m = (e >> 4) % a.T, v = (e >> 4) / a.T;
+  for (int e = warp; e < pairs; e += kExpertWarps) {
+    const int v = e / a.T, m = e - v * a.T;
     float s = 0.0f;
-    for (int i = 0; i < split; ++i) s = __fadd_rn(s, sums[((v * split + i) * a.T + m) * 17 + k]);
-    if (S > 1) sums[(v * split * a.T + m) * 17 + k] = s;
-    else finish(v, m, k, s);
+    for (int i = 0; i < split; ++i) s = __fadd_rn(s, sums[((v * split + i) * a.T + m) * 33 + lane]);
+    if (S > 1) sums[(v * split * a.T + m) * 33 + lane] = s;
+    else finish(v, m, s);
   }
   if (S == 1) return;
   cluster.sync();
-  for (int e = threadIdx.x * S + rank; e < outputs; e += kExpertWarps * 32 * S) {
-    const int k = e & 15, m = (e >> 4) % a.T, v = (e >> 4) / a.T;
-    float s = 0.0f;
-    for (int b = 0; b < S; ++b) s = __fadd_rn(s, cluster.map_shared_rank(sums, b)[(v * split * a.T + m) * 17 + k]);
-    finish(v, m, k, s);
+  for (int e = warp * S + rank; e < pairs; e += kExpertWarps * S) {
+    const int v = e / a.T, m = e - v * a.T;
+    float s = 0.0f, of[kDownCluster];
+#pragma unroll
+    for (int b = 0; b < kDownCluster; ++b) of[b] = b < S ? cluster.map_shared_rank(sums, b)[(v * split * a.T + m) * 33 + lane] : 0.0f;
+#pragma unroll
+    for (int b = 0; b < kDownCluster; ++b) s = __fadd_rn(s, of[b]);
+    finish(v, m, s);
   }
   cluster.sync();   // no block leaves while another reads its sums
 }
 
 namespace {
 
-#ifndef UPBLOCKS
-#define UPBLOCKS 2
-#endif
-#ifndef DOWNBLOCKS
-#define DOWNBLOCKS 2
-#endif
+constexpr long kBlocksPerSm = 2;    // of both products: more of them only start more often
 // spread_smem for blocks that have Lists in static shared memory besides.
 size_t spread_beside_lists(size_t smem, int per) {
   const size_t all = spread_smem(smem + sizeof(Lists), per);
@@ -514,9 +517,9 @@ template <bool VEC, int DT, int NT, bool SMALL, bool ZEROS>
 int launch_up(const ExpertsArgs& a, long slots, int num_sms, int dev, cudaStream_t st) {
   constexpr size_t least = (size_t)kExpertWarps * (kUpDepth * Ring<2, 1, SMALL, ZEROS>::kSlot + NT * 8 * 33 * sizeof(float));
   const long tiles_K = (a.I + 15) / 16;
-  const int split = shared_by(tiles_K * slots, a.gate.tiles_C, kExpertWarps, (long)UPBLOCKS * kExpertWarps * num_sms);
+  const int split = shared_by(tiles_K * slots, a.gate.tiles_C, kExpertWarps, kBlocksPerSm * kExpertWarps * num_sms);
   const long items = (tiles_K + kExpertWarps / split - 1) / (kExpertWarps / split) * slots;
-  const long most = (long)UPBLOCKS * num_sms, blocks = items < most ? items : most;
+  const long most = kBlocksPerSm * num_sms, blocks = items < most ? items : most;
   const size_t smem = spread_beside_lists(least, (int)((blocks + num_sms - 1) / num_sms));
   static DeviceOnce once;
   auto kernel = k_experts_up<VEC, DT, NT, SMALL, ZEROS>;
@@ -527,19 +530,28 @@ int launch_up(const ExpertsArgs& a, long slots, int num_sms, int dev, cudaStream
 
 template <int P, int NT, bool SMALL, bool ZEROS>
 int launch_down(const ExpertsArgs& a, long slots, int num_sms, int dev, cudaStream_t st) {
-  constexpr size_t ring = (size_t)kExpertWarps * kDownDepth * Ring<1, 1, SMALL, ZEROS>::kSlot;
-  const long tiles_K = (a.D + 15) / 16;
-  const int by = shared_by(tiles_K, (a.I + 127l) / 128 * slots, 8 * kExpertWarps, (long)DOWNBLOCKS * kExpertWarps * num_sms);
+  constexpr size_t ring = (size_t)kExpertWarps * kDownDepth * Ring<2, 1, SMALL, ZEROS>::kSlot;
+  const long units = ((a.D + 15) / 16 + 1) / 2;
+  const int by = shared_by(units, (a.I + 127l) / 128 * slots, kDownCluster * kExpertWarps, kBlocksPerSm * kExpertWarps * num_sms);
   const int split = by < kExpertWarps ? by : kExpertWarps, S = by / split;
-  const long blocks = (tiles_K + kExpertWarps / split - 1) / (kExpertWarps / split);
+  const long blocks = (units + kExpertWarps / split - 1) / (kExpertWarps / split);
   const long per_sm = (blocks * S + num_sms - 1) / num_sms;
-  const size_t smem = spread_beside_lists(ring + (size_t)kExpertWarps * a.T * 17 * sizeof(float), per_sm <= 8 ? (int)per_sm : 0);
+  const size_t smem = spread_beside_lists(ring + (size_t)kExpertWarps * a.T * 33 * sizeof(float), per_sm <= 8 ? (int)per_sm : 0);
   static DeviceOnce once;
   auto kernel = k_experts_down<P, NT, SMALL, ZEROS>;
-  const int rc = set_max_smem(once, dev, kernel, spread_beside_lists(ring + (size_t)kExpertWarps * kSliceTokens * 17 * sizeof(float), 1));
+  const int rc = set_max_smem(once, dev, kernel, spread_beside_lists(ring + (size_t)kExpertWarps * kSliceTokens * 33 * sizeof(float), 1));
   if (rc != 0) return rc;
   return launch_kernel_cluster(kernel, dim3((unsigned)(blocks * S)), dim3(kExpertWarps * 32), (unsigned)S, smem, st,
                                true, a, split);
+}
+
+template <int P, int NT>
+int launch_down_groups(const ExpertsArgs& a, long slots, int num_sms, int dev, cudaStream_t st) {
+  if (a.down.zeros)
+    return a.down.group < 128 ? launch_down<P, NT, true, true>(a, slots, num_sms, dev, st)
+                              : launch_down<P, NT, false, true>(a, slots, num_sms, dev, st);
+  return a.down.group < 128 ? launch_down<P, NT, true, false>(a, slots, num_sms, dev, st)
+                            : launch_down<P, NT, false, false>(a, slots, num_sms, dev, st);
 }
 
 template <int DT, int NT>
@@ -559,9 +571,10 @@ int launch_slice(const ExpertsArgs& a, int num_sms, cudaStream_t st) {
                 : (a.gate.group < 128 ? (a.gate.zeros ? launch_up<false, DT, NT, true, true> : launch_up<false, DT, NT, true, false>)
                                       : (a.gate.zeros ? launch_up<false, DT, NT, false, true> : launch_up<false, DT, NT, false, false>));
   if ((rc = up(a, slots, num_sms, dev, st)) != 0) return rc;
-  auto down = a.down.group < 128 ? (a.down.zeros ? launch_down<P, NT, true, true> : launch_down<P, NT, true, false>)
-                                 : (a.down.zeros ? launch_down<P, NT, false, true> : launch_down<P, NT, false, false>);
-  return down(a, slots, num_sms, dev, st);
+  // columns for as many tokens as an expert may have of very few, else for more than it has as a rule: a
+  // warp whose experts have more multiplies again, and the others wait for it
+  if (NT == 1 && a.T <= (P == 2 ? 4 : 2)) return launch_down_groups<P, 1>(a, slots, num_sms, dev, st);
+  return launch_down_groups<P, NT == 1 ? 2 : 4>(a, slots, num_sms, dev, st);
 }
 
 template <int DT>

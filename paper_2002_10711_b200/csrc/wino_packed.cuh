@@ -195,17 +195,6 @@ template <> struct Input<WINO_INT8> {
   }
 };
 
-// P planes of bf16 whose sum is the input (of the second product of an experts layer).
-template <int P> struct Planes {
-  static constexpr int kParts = P;
-  static constexpr bool kF16 = false;
-  uint4 v[P];
-  __device__ __forceinline__ void operand(int, uint32_t (&b)[P][4]) const {
-#pragma unroll
-    for (int p = 0; p < P; ++p) { b[p][0] = v[p].x; b[p][1] = v[p].y; b[p][2] = v[p].z; b[p][3] = v[p].w; }
-  }
-};
-
 // The eight values of an input of real type.
 template <int DT>
 __device__ __forceinline__ void to_floats(const Input<DT>& in, float (&v)[8]) {
