@@ -81,21 +81,26 @@ k_experts_route(const __grid_constant__ ExpertsArgs a) {
 #pragma unroll
       for (int i = 0; i < 8; ++i) s = __fmaf_rn(xv[i], rv[i], s);
     };
-    int k = lane * 8;
-    if (a.vec && a.vec_router)
+    if (a.vec && a.vec_router && a.D % 8 == 0) {
 #pragma unroll 1
-      for (; k + 3 * 256 + 8 <= a.D; k += 4 * 256) {
+      for (int k = lane * 8; k < a.D; k += 4 * 256) {      // four loads of each on the way at a time
         In xi[4], ri[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          xi[i].load(x + (k + 256 * i) * In::kBytes);
-          ri[i].load(r + (k + 256 * i) * In::kBytes);
+          xi[i].clear(0);
+          ri[i].clear(0);
+          if (k + 256 * i < a.D) {
+            xi[i].load(x + (k + 256 * i) * In::kBytes);
+            ri[i].load(r + (k + 256 * i) * In::kBytes);
+          }
         }
 #pragma unroll
         for (int i = 0; i < 4; ++i) add(xi[i], ri[i]);
       }
+    } else {
 #pragma unroll 1
-    for (; k < a.D; k += 256) add(load_input<DT>(x, k, a.D, a.vec, 0), load_input<DT>(r, k, a.D, a.vec_router, 0));
+      for (int k = lane * 8; k < a.D; k += 256) add(load_input<DT>(x, k, a.D, a.vec, 0), load_input<DT>(r, k, a.D, a.vec_router, 0));
+    }
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) s = __fadd_rn(s, __shfl_xor_sync(0xffffffffu, s, o));
     if (waits) cluster.barrier_wait(std::move(arrived)), waits = false;
@@ -559,9 +564,9 @@ int launch_slice(const ExpertsArgs& a, int num_sms, cudaStream_t st) {
   constexpr int P = Input<DT>::kParts == 3 ? 3 : 2;
   int dev = 0;
   if (cudaGetDevice(&dev) != cudaSuccess) return WINO_ERR_CUDA;
-  // blocks that share a token's experts, eight or more each, while there are SMs for them
+  // blocks that share a token's experts, until a warp has one, while there are SMs for them
   int S = 1;
-  while (S < 8 && (long)a.T * S * 2 <= num_sms && S * 2 * (kRouteThreads / 32) <= a.E) S *= 2;
+  while (S < 8 && (long)a.T * S * 2 <= num_sms && S * (kRouteThreads / 32) < a.E) S *= 2;
   int rc = launch_kernel_cluster(k_experts_route<DT>, dim3((unsigned)(a.T * S)), dim3(kRouteThreads), (unsigned)S, 0, st, true, a);
   if (rc != 0) return rc;
   const long slots = (long)a.T * a.top_k < a.E ? (long)a.T * a.top_k : a.E;
