@@ -277,9 +277,9 @@ typedef struct {
 int wino_direct_conv_forward(const wino_direct_desc_t* desc, const int8_t* x_NHWC_dev,
                              const int8_t* w_KRSC_dev, const float* bias_K_dev, void* y_dev,
                              void* stream);
-/* Status of the direct convolutions on the current device, which have no plan to keep
- * one in: synchronizes `stream`, returns WINO_OK, WINO_ERR_TIMEOUT (a bounded wait
- * inside the tensor-core kernel expired; its output is undefined) or WINO_ERR_CUDA,
+/* Status of the direct convolutions and of the linear layers with 4-bit weights on the current
+ * device, which have no plan to keep one in: synchronizes `stream`, returns WINO_OK, WINO_ERR_TIMEOUT
+ * (a bounded wait inside a tensor-core kernel expired; its output is undefined) or WINO_ERR_CUDA,
  * and clears the word. */
 int wino_direct_last_status(void* stream);
 
@@ -323,7 +323,8 @@ size_t wino_packed_scale_count(int32_t K, int32_t C, int32_t group);
  *   scale = round((hi - lo) / 15), zero = clamp(rne(-lo / scale), 0, 15);
  *   code = clamp(rne(w / scale) + zero, 0, 15)
  * in 32-bit floats, scales rounded to scale_dtype and at most its largest value; where the scale is 0, zero = code = 8.
- * Rows beyond K get scale 0, zero 8, code 8.  w has to be finite (else: codes and scales without meaning).
+ * Rows beyond K get scale 0, zero 8, code 8.  w has to be finite (else: codes and scales without meaning), and no
+ * buffer may overlap another.
  * values_dev (nullable): dense [K][C] of w's type, the values that the codes stand for, rounded once. */
 int wino_quantize_weights(const wino_packed_t* out, const void* w_dev, int32_t w_dtype, int64_t w_stride,
                           void* values_dev, void* stream);
@@ -332,7 +333,7 @@ int wino_quantize_weights(const wino_packed_t* out, const void* w_dev, int32_t w
  * point) is read for WINO_INT8 only.  y [M][K], rows y_stride elements apart, of y_dtype; for WINO_INT8
  * through q_Y as everywhere in this library: Q(fmaf(sum, s_x/s_Y, bias/s_Y); 1).  Rows of x and y need the
  * alignment of their elements only (16 bytes and multiples of 16 are faster).  M = 0 is no work.
- * Elements of y between rows are left as they are. */
+ * Elements of y between rows are left as they are; y may not overlap x. */
 typedef struct {
   int32_t M, x_dtype, y_dtype;
   int64_t x_stride, y_stride;
@@ -353,8 +354,9 @@ int wino_linear_forward(const wino_linear_desc_t* desc, const void* x_dev, const
  * ids are the lowest experts that are out, with weight 0.  A NaN or +inf among a token's logits makes its weights and y NaN.
  * ids int32 [T][top_k] and weights float [T][top_k] receive S, largest first, and a.
  * E <= 512, top_k <= 16.  Any T; the layer is laid out for few tokens (up to 64 go through the experts at
- * once, and an expert's weights are read once for up to 16 of its tokens).  T = 0 is no work.
- * workspace_dev: wino_experts_workspace_bytes, 16-byte aligned, not shared by calls that may overlap. */
+ * once, and an expert's weights are read once for 8 or, where it has more, 16 of its tokens).  T = 0 is no work.
+ * y may not overlap x.  workspace_dev: wino_experts_workspace_bytes, 16-byte aligned, not shared by calls that
+ * may overlap. */
 typedef struct {
   int32_t T, D, I, E, top_k, normalize, dtype;
   int64_t x_stride, y_stride;

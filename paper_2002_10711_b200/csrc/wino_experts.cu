@@ -252,7 +252,7 @@ __device__ __forceinline__ void build_lists(Lists& l, const ExpertsArgs& a) {
 }
 
 // ---- gate and up --------------------------------------------------------------------------
-constexpr int kUpDepth = 3, kDownDepth = 3, kDownCluster = 8;
+constexpr int kUpDepth = 3, kDownDepth = 3, kDownCluster = 4;
 
 // An item is an expert, 8 / split row tiles, and 8 NT of the expert's tokens; a block takes every
 // gridDim.x-th, and has the next one's first tiles on the way while it finishes one.

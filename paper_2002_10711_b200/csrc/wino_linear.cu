@@ -158,9 +158,6 @@ int launch_type(const LinearArgs& a, int num_sms, cudaStream_t st) {
 }
 
 }  // namespace
-#ifndef TCMIN
-#define TCMIN 9
-#endif
 int launch_linear(const wino_linear_desc_t& d, const void* x, const float* bias, void* y, int num_sms,
                   cudaStream_t st) {
   LinearArgs a;
@@ -179,7 +176,12 @@ int launch_linear(const wino_linear_desc_t& d, const void* x, const float* bias,
   a.out.z_Y = codes ? d.q_Y.zero_point : 0;
   a.out.lo = codes ? (float)(d.q_Y.qmin - d.q_Y.zero_point) : 0.0f;
   a.out.hi = codes ? (float)(d.q_Y.qmax - d.q_Y.zero_point) : 0.0f;
-  if (linear_tc_supported(a, d.x_dtype) && d.M >= TCMIN) {
+  // The tcgen05 kernel takes some 2 us longer to start and to finish, and less for every weight: a warp MMA
+  // goes through the weights once for every 16 rows of x.  us, this / that:  16 rows 8192x8192 16.4 / 15.1,
+  // 4096x4096 7.4 / 7.4, 1024x1024 3.5 / 5.0;  32 rows 4096x4096 9.1 / 7.9, 1024 -> 8192 6.9 / 6.7;  64 rows
+  // 1024 -> 8192 11.8 / 8.1, 512x512 4.1 / 6.7;  8 rows 8192x8192 12.9 / 14.8.
+  const double passes = (d.M + 15) / 16, work = passes * d.w.K * d.w.C;
+  if (linear_tc_supported(a, d.x_dtype) && d.M > 8 && work >= (passes == 1 ? 50e6 : 20e6)) {
     int dev = 0;
     if (cudaGetDevice(&dev) != cudaSuccess) return WINO_ERR_CUDA;
     return launch_linear_tc(a, d.x_dtype, num_sms, dev, st);

@@ -353,9 +353,11 @@ template <bool F16, int NP, bool SMALL, bool ZEROS>
 int launch_tc(const LinearArgs& a, int num_sms, int device, int* status, cudaStream_t st) {
   const long blocks = (a.w.K + 127) / 128, slices = (a.M + NP - 1) / NP;
   if (slices > 65535) return WINO_ERR_UNSUPPORTED;
-  // blocks that share the inputs, while there are SMs for them and two chunks for each
+  // blocks that share the inputs, while there are SMs for them and two chunks for each; of clusters of more than
+  // four, one to an SM, the GPU holds no more than fourteen at once (2048 x 2048: 10 us in sixteen of eight)
+  const int most = blocks * slices <= 14 ? 8 : 4;
   int S = 1;
-  while (S < 8 && blocks * slices * (S + 1) <= num_sms && (S + 1) * 2 <= a.w.tiles_C) ++S;
+  while (S < most && blocks * slices * (S + 1) <= num_sms && (S + 1) * 2 <= a.w.tiles_C) ++S;
   constexpr size_t ring = (size_t)kRing * NP * 256 + tc_sets(NP) * kTcStages * kStageBytes + kEpiWarps * kScaleStages * 64;
   constexpr size_t sums = (size_t)NP * 128 * sizeof(float);
   constexpr size_t smem = (ring > sums ? ring : sums) + 1024;

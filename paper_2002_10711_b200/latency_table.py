@@ -4,7 +4,7 @@ This is the lookup table a latency-aware search over convolution algorithms
 needs (paper: Section 4, "each candidate operation comes with its respective
 latency"); the paper filled it on Arm cores.
 
-    python -m paper_2002_10711_b200.latency_table [--batch 256] [--channels 256] [--strided]
+    python -m paper_2002_10711_b200.latency_table [--batch 256] [--channels 256] [--strided] [--head]
 
 The direct convolution is the library's implicit GEMM on the tensor cores (stride 1,
 channel counts that are multiples of 64 / 32; other layers run on the integer ALUs).
@@ -90,17 +90,34 @@ def strided_latency(N, C, H, W, K, device="cuda:0", sets=8):
     return t
 
 
+def head_latency(N, C, K, device="cuda:0", sets=8):
+    """Microseconds per call of the network's classifier, C pooled int8 codes -> K classes, with 4-bit weights."""
+    from . import layer
+    dev = torch.device(device)
+    gen = torch.Generator(device="cpu").manual_seed(3)
+    xs = [torch.randint(0, 127, (N, C), dtype=torch.int8, generator=gen).to(dev) for _ in range(sets)]
+    ys = [torch.empty((N, K), dtype=torch.float32, device=dev) for _ in range(sets)]
+    w = layer.quantize_w4(torch.randn((K, C), generator=gen).to(dev), 64)
+    bias = torch.randn(K, generator=gen).to(dev)
+    return _time_graph(lambda i: layer.linear_w4(xs[i % sets], w, bias, dict(scale=0.05), out=ys[i % sets]))
+
+
 def main():
     ap = argparse.ArgumentParser()
     ap.add_argument("--batch", type=int, default=256)
     ap.add_argument("--channels", type=int, default=0, help="only the layer shape of this width")
     ap.add_argument("--strided", action="store_true",
                     help="also the network's three stride-2 layers (direct convolution only)")
+    ap.add_argument("--head", action="store_true", help="also the network's classifier, with 4-bit weights")
     args = ap.parse_args()
     if args.strided:
         for (C, S), (K, _) in zip(RESNET18_CIFAR[:-1], RESNET18_CIFAR[1:]):
             print(json.dumps({"N": args.batch, "C": C, "K": K, "H": S, "W": S, "stride": 2,
                               "us": {"direct": round(strided_latency(args.batch, C, S, S, K), 1)}}), flush=True)
+    if args.head:
+        C = RESNET18_CIFAR[-1][0]
+        print(json.dumps({"N": args.batch, "C": C, "K": 10, "us": {"linear_w4": round(head_latency(args.batch, C, 10), 1)}}),
+              flush=True)
     for C, S in RESNET18_CIFAR:
         if args.channels and C != args.channels:
             continue

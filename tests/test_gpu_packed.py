@@ -76,6 +76,58 @@ def test_linear_large(M, C, K, dtype):
     _linear_case(M, C, K, 128, dtype, True)
 
 
+@pytest.mark.parametrize("dtype", [BF, HF])
+@pytest.mark.parametrize("M,C,K,group,zeros,bias", [
+    (13, 8200, 6200, 128, True, True),          # one pass of 16 rows, sizes that fill no tile
+    (16, 6184, 8201, 64, False, False),
+    (9, 16384, 3200, 16384, True, False),       # a scale for each output
+    (20, 3336, 3100, 32, True, True),
+    (32, 4096, 2561, 128, False, True),
+    (40, 2568, 2700, 256, True, False),
+    (64, 2048, 2600, 128, False, False),
+    (64, 1032, 5000, 32, True, True),
+    (65, 1160, 3500, 384, True, True),
+    (130, 904, 2500, 64, False, True),
+    (300, 128, 8300, 128, True, False),         # a single chunk of inputs
+    (1000, 72, 4500, 128, False, True),
+])
+def test_linear_many_rows(M, C, K, group, zeros, bias, dtype):
+    assert -(-M // 16) * K * C >= (50e6 if M <= 16 else 20e6)      # sizes that the tcgen05 kernel takes
+    _linear_case(M, C, K, group, dtype, zeros, bias, HF if K % 2 else BF)
+    assert binding.direct_last_status() == 0
+
+
+def test_linear_many_rows_strided_and_infinite():
+    rng = np.random.default_rng(31)
+    M, C, K, group = 70, 1160, 3600, 128
+    w, W = _weights(rng, K, C, group, BF, True)
+    base = _inputs(rng, (M + 1, C + 24), BF).cuda()
+    x = base[1:, 8:8 + C]                                 # rows on 16-byte boundaries inside a larger buffer
+    room = torch.full((M, K + 9), 7.0, dtype=BF, device="cuda")
+    layer.linear_w4(x, w, out=room[:, 5:5 + K])
+    assert (room[:, :5] == 7).all() and (room[:, 5 + K:] == 7).all()
+    want, bound = ref.linear(x.double().cpu(), W, None, group)
+    _check(room[:, 5:5 + K], want, bound, BF)
+    clean = room[:, 5:5 + K].cpu()
+    bad = x.clone()
+    bad[3, 7], bad[69, 1159], bad[64, 0] = float("nan"), float("inf"), float("-inf")
+    y = layer.linear_w4(bad, w).cpu()
+    rest = [m for m in range(M) if m not in (3, 64, 69)]
+    assert torch.equal(y[rest], clean[rest])
+    want = bad.double().cpu() @ W.T
+    for m in (3, 64, 69):
+        assert torch.equal(torch.isnan(y[m]), torch.isnan(want[m]))
+        fine = ~torch.isnan(want[m])
+        assert (torch.sign(y[m].double())[fine] == torch.sign(want[m])[fine]).all()
+    # unaligned rows of the same values go another way to the same place
+    odd = base.flatten()[1:1 + M * C].view(M, C).clone()
+    shifted = torch.empty(M * C + 1, dtype=BF, device="cuda")[1:].view(M, C)
+    shifted.copy_(odd)
+    want, bound = ref.linear(odd.double().cpu(), W, None, group)
+    _check(layer.linear_w4(shifted, w), want, bound, BF)
+    _check(layer.linear_w4(odd, w), want, bound, BF)
+
+
 @pytest.mark.parametrize("M", [1, 3, 20, 150])
 @pytest.mark.parametrize("dtype", [BF, HF, F32, I8])
 def test_linear_strides_and_alignment(M, dtype):
@@ -366,10 +418,11 @@ def test_same_bits_every_time_on_streams_and_in_graphs():
     head, _ = _weights(rng, 100, D, 64)
     router = torch.from_numpy(rng.normal(0, 1, (E, D)) / 16).to(BF).cuda()
     xs = [_inputs(rng, (M, D), BF).cuda() for M in (1, 4, 20)]
+    wide, _ = _weights(rng, 40000, D, 64)                  # twenty rows: the tcgen05 kernel
 
     def run(x):
         y, ids, w = layer.experts_w4(x, router, gate, up, down, 4)
-        return y, ids, w, layer.linear_w4(y, head)
+        return y, ids, w, layer.linear_w4(y, head), layer.linear_w4(y, wide)
     want = [run(x) for x in xs]
     torch.cuda.synchronize()
     streams = [torch.cuda.Stream() for _ in xs]
@@ -492,3 +545,8 @@ def test_a_network_with_its_head():
                                       (32, 32), 2, True, F32)
     assert torch.equal(ids.cpu().long(), order)
     _check(out, want, off + 8 * ref.U * want.abs().max(), F32)
+
+
+def test_latency_table_has_the_head():
+    from paper_2002_10711_b200 import latency_table
+    assert latency_table.head_latency(2, 64, 10, sets=2) > 0
