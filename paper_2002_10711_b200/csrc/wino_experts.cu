@@ -258,7 +258,7 @@ constexpr int kUpDepth = 3, kDownDepth = 3, kDownCluster = 4;
 // gridDim.x-th, and has the next one's first tiles on the way while it finishes one.
 template <bool VEC, int DT, int NT, bool SMALL, bool ZEROS>
 __global__ void __launch_bounds__(kExpertWarps * 32)
-k_experts_up(const __grid_constant__ ExpertsArgs a, int split) {
+k_experts_up(const __grid_constant__ ExpertsArgs a, int log_split) {
   using In = Input<DT>;
   using Tiles = Ring<2, 1, SMALL, ZEROS>;
   constexpr int P = In::kParts == 3 ? 3 : 2;
@@ -267,22 +267,24 @@ k_experts_up(const __grid_constant__ ExpertsArgs a, int split) {
   float* sums = reinterpret_cast<float*>(smem + kExpertWarps * kUpDepth * Tiles::kSlot);   // [warp][token][33]
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
   griddep_launch();
-  griddep_wait();
-  build_lists(lists, a);
-  const int tiles_K = (a.I + 15) / 16, per_block = kExpertWarps / split, blocks_K = (tiles_K + per_block - 1) / per_block;
-  const int part = warp % split;
-  const int c0 = (int)((long)a.gate.tiles_C * part / split), c1 = (int)((long)a.gate.tiles_C * (part + 1) / split);
+  // what needs no lists, before the wait
+  const int split = 1 << log_split;
+  const int tiles_K = (a.I + 15) / 16, per_block = kExpertWarps >> log_split, blocks_K = (tiles_K + per_block - 1) / per_block;
+  const int part = warp & (split - 1);
+  const int c0 = (int)((long)a.gate.tiles_C * part >> log_split), c1 = (int)((long)a.gate.tiles_C * (part + 1) >> log_split);
   const uint32_t ring = smem_u32(smem) + warp * kUpDepth * Tiles::kSlot, ring_end = ring + kUpDepth * Tiles::kSlot;
   int slot = blockIdx.x / blocks_K, block_K = blockIdx.x - slot * blocks_K, n0 = 0;
+  griddep_wait();
+  build_lists(lists, a);
   Tiles tiles;
   auto begin = [&]() {
     if (slot < lists.chosen) {
-      const int tile_K = min(block_K * per_block + warp / split, tiles_K - 1), expert = lists.expert[slot];
+      const int tile_K = min(block_K * per_block + (warp >> log_split), tiles_K - 1), expert = lists.expert[slot];
       const Stream from[2] = {stream_of(expert_of(a.gate, expert, a.gate_units, a.gate_scales), tile_K),
                               stream_of(expert_of(a.up, expert, a.gate_units, a.gate_scales), tile_K)};
       tiles.start(from, a.gate, c0, c1, lane);
     }
-#pragma unroll
+#pragma unroll 1                  // (code that runs once is waited for, about ten cycles an instruction)
     for (int d = 0; d < kUpDepth; ++d) {
       if (slot < lists.chosen && c0 + d < c1) tiles.fill(ring + d * Tiles::kSlot, lane);
       Tiles::commit();
@@ -362,7 +364,7 @@ k_experts_up(const __grid_constant__ ExpertsArgs a, int split) {
 // MMA are four tokens' upper parts and their lower ones, added up at the end.
 template <int P, int NT, bool SMALL, bool ZEROS>
 __global__ void __launch_bounds__(kExpertWarps * 32)
-k_experts_down(const __grid_constant__ ExpertsArgs a, int split) {
+k_experts_down(const __grid_constant__ ExpertsArgs a, int log_split, int log_S) {
   using In = Input<WINO_BF16>;
   using Tiles = Ring<2, 1, SMALL, ZEROS>;
   constexpr int kEach = P == 2 ? 4 : 2, kTokens = NT * kEach;      // tokens of an MMA's columns, and at a time
@@ -374,15 +376,15 @@ k_experts_down(const __grid_constant__ ExpertsArgs a, int split) {
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
   griddep_launch();
   for (int e = threadIdx.x; e < kExpertWarps * a.T * 33; e += blockDim.x) sums[e] = 0.0f;
+  float* mine = sums + warp * a.T * 33;
+  const int split = 1 << log_split, per_block = kExpertWarps >> log_split, tiles_K = (a.D + 15) / 16, tiles = a.down.tiles_C;
+  const int unit = (int)(blockIdx.x >> log_S) * per_block + (warp >> log_split);     // two row tiles
+  const int part = rank * split + (warp & (split - 1)), log_by = log_split + log_S;
   griddep_wait();
   build_lists(lists, a);
-  float* mine = sums + warp * a.T * 33;
-  const int per_block = kExpertWarps / split, tiles_K = (a.D + 15) / 16, tiles = a.down.tiles_C;
-  const int unit = (int)(blockIdx.x / S) * per_block + warp / split;            // two row tiles
   // this warp's part of the tiles of all chosen experts, [expert][tile of inputs]
-  const int part = rank * split + warp % split, shared_by = split * S;
   const int all = lists.chosen * tiles;
-  const int u0 = (int)((long)all * part / shared_by), u1 = unit * 2 < tiles_K ? (int)((long)all * (part + 1) / shared_by) : u0;
+  const int u0 = (int)((long)all * part >> log_by), u1 = unit * 2 < tiles_K ? (int)((long)all * (part + 1) >> log_by) : u0;
   const uint32_t ring = smem_u32(smem) + warp * kDownDepth * Tiles::kSlot, ring_end = ring + kDownDepth * Tiles::kSlot;
   int slot = 0, c = 0, fill_slot = 0, fill_c = 0;
   Tiles from;
@@ -477,7 +479,7 @@ k_experts_down(const __grid_constant__ ExpertsArgs a, int split) {
   // unit; a cluster's blocks leave their sums where their first warp's were.
   const int pairs = per_block * a.T;
   auto finish = [&](int v, int m, float s) {
-    const long out = ((long)(blockIdx.x / S) * per_block + v) * 32 + lane;
+    const long out = ((long)(blockIdx.x >> log_S) * per_block + v) * 32 + lane;
     if (out < a.D) store_output(a.out, m * a.y_row + out, s, 0.0f);
   };
   for (int e = warp; e < pairs; e += kExpertWarps) {
@@ -518,6 +520,12 @@ int shared_by(long row_tiles, long tiles, int most, long warps) {
   return n;
 }
 
+int log2_of(int n) {
+  int l = 0;
+  while (1 << l < n) ++l;
+  return l;
+}
+
 template <bool VEC, int DT, int NT, bool SMALL, bool ZEROS>
 int launch_up(const ExpertsArgs& a, long slots, int num_sms, int dev, cudaStream_t st) {
   constexpr size_t least = (size_t)kExpertWarps * (kUpDepth * Ring<2, 1, SMALL, ZEROS>::kSlot + NT * 8 * 33 * sizeof(float));
@@ -530,7 +538,7 @@ int launch_up(const ExpertsArgs& a, long slots, int num_sms, int dev, cudaStream
   auto kernel = k_experts_up<VEC, DT, NT, SMALL, ZEROS>;
   const int rc = set_max_smem(once, dev, kernel, spread_beside_lists(least, 1));
   if (rc != 0) return rc;
-  return launch_kernel(kernel, dim3((unsigned)blocks), dim3(kExpertWarps * 32), smem, st, true, a, split);
+  return launch_kernel(kernel, dim3((unsigned)blocks), dim3(kExpertWarps * 32), smem, st, true, a, log2_of(split));
 }
 
 template <int P, int NT, bool SMALL, bool ZEROS>
@@ -547,7 +555,7 @@ int launch_down(const ExpertsArgs& a, long slots, int num_sms, int dev, cudaStre
   const int rc = set_max_smem(once, dev, kernel, spread_beside_lists(ring + (size_t)kExpertWarps * kSliceTokens * 33 * sizeof(float), 1));
   if (rc != 0) return rc;
   return launch_kernel_cluster(kernel, dim3((unsigned)(blocks * S)), dim3(kExpertWarps * 32), (unsigned)S, smem, st,
-                               true, a, split);
+                               true, a, log2_of(split), log2_of(S));
 }
 
 template <int P, int NT>

@@ -49,7 +49,7 @@ k_linear_rows(const __grid_constant__ LinearArgs a) {
     const uint32_t ring = smem_u32(smem) + warp * kRingSlots * Tiles::kSlot, ring_end = ring + kRingSlots * Tiles::kSlot;
     Tiles tiles;
     tiles.start(w, a.w, c0, c1, lane);
-#pragma unroll
+#pragma unroll 1
     for (int d = 0; d < kRingSlots; ++d) {
       if (c0 + d < c1) tiles.fill(ring + d * Tiles::kSlot, lane);
       Tiles::commit();
