@@ -66,6 +66,8 @@ k_experts_route(const __grid_constant__ ExpertsArgs a) {
   // (behind the last expert: for four at a time)
   if (rank == 0)
     for (int e = a.E + threadIdx.x; e < (a.E + 3) / 4 * 4; e += kRouteThreads) logits[e] = -INFINITY;
+  int log_by = 0;          // 2^log_by neighbouring lanes rank one expert
+  while (log_by < 5 && a.E << (log_by + 1) <= kRouteThreads) ++log_by;
   auto arrived = cluster.barrier_arrive();         // the first block is there to be written to: waited for below
   griddep_wait();
   const char* x = a.x + token * a.x_row;
@@ -82,11 +84,12 @@ k_experts_route(const __grid_constant__ ExpertsArgs a) {
       for (int i = 0; i < 8; ++i) s = __fmaf_rn(xv[i], rv[i], s);
     };
     if (a.vec && a.vec_router && a.D % 8 == 0) {
+      constexpr int kAtOnce = DT == WINO_FLOAT ? 4 : 8;     // loads of each on the way at a time
 #pragma unroll 1
-      for (int k = lane * 8; k < a.D; k += 4 * 256) {      // four loads of each on the way at a time
-        In xi[4], ri[4];
+      for (int k = lane * 8; k < a.D; k += kAtOnce * 256) {
+        In xi[kAtOnce], ri[kAtOnce];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
+        for (int i = 0; i < kAtOnce; ++i) {
           xi[i].clear(0);
           ri[i].clear(0);
           if (k + 256 * i < a.D) {
@@ -95,7 +98,7 @@ k_experts_route(const __grid_constant__ ExpertsArgs a) {
           }
         }
 #pragma unroll
-        for (int i = 0; i < 4; ++i) add(xi[i], ri[i]);
+        for (int i = 0; i < kAtOnce; ++i) add(xi[i], ri[i]);
       }
     } else {
 #pragma unroll 1
@@ -110,26 +113,23 @@ k_experts_route(const __grid_constant__ ExpertsArgs a) {
   cluster.sync();
   if (rank != 0) return;
   bool odd = false;                       // NaN or +inf
-  for (int e = threadIdx.x; e < a.E; e += kRouteThreads) odd |= !(logits[e] < INFINITY);
-  odd = __syncthreads_or(odd);
-  // `by` neighbouring lanes count for one expert
-  int by = 1;
-  while (by < 32 && a.E * by * 2 <= kRouteThreads) by *= 2;
-  for (int e0 = 0; e0 < a.E; e0 += kRouteThreads / by) {
-    const int e = e0 + threadIdx.x / by, part = threadIdx.x % by;
+  for (int e0 = 0; e0 < a.E; e0 += kRouteThreads >> log_by) {
+    const int e = e0 + (threadIdx.x >> log_by), part = threadIdx.x & ((1 << log_by) - 1);
     const float l = e < a.E ? logits[e] : 0.0f;
+    odd |= !(l < INFINITY);
     int place = 0;
-    for (int f = part * 4; f < a.E; f += by * 4) {
+    for (int f = part * 4; f < a.E; f += 4 << log_by) {
       const float4 o = *reinterpret_cast<const float4*>(logits + f);
       place += o.x > l || (o.x == l && f < e);
       place += o.y > l || (o.y == l && f + 1 < e);
       place += o.z > l || (o.z == l && f + 2 < e);
       place += o.w > l || (o.w == l && f + 3 < e);
     }
-    for (int o = 1; o < by; o *= 2) place += __shfl_xor_sync(0xffffffffu, place, o);
-    if (part == 0 && e < a.E && place < a.top_k && !odd) top_l[place] = l, top_e[place] = e;
+    for (int o = 1; o < 1 << log_by; o *= 2) place += __shfl_xor_sync(0xffffffffu, place, o);
+    // (with a NaN about, places mean nothing, and nothing is done with them)
+    if (part == 0 && e < a.E && place < a.top_k) top_l[place] = l, top_e[place] = e;
   }
-  __syncthreads();
+  odd = __syncthreads_or(odd);
   if (warp != 0) return;
   const bool mine = lane < a.top_k;
   if (odd) {
