@@ -152,6 +152,7 @@ wino_packed_t packed(PyObject* o, long batch, const at::Device& device) {
     refuse(PyExc_ValueError, "scales must be contiguous bfloat16 or float16 [..., K/16, groups, 16]");
   if (codes.device() != device || scales.device() != device)
     refuse(PyExc_ValueError, "packed weights must be on the device of the input");
+  forward_only(scales);
   w.codes_dev = codes.const_data_ptr();
   w.scales_dev = scales.const_data_ptr();
   w.zeros_dev = nullptr;
@@ -188,8 +189,17 @@ Rows rows_of(const at::Tensor& x, int64_t n, at::Tensor& keep) {
   if (r.count > (1 << 24)) refuse(PyExc_ValueError, "more than 2^24 rows");
   return r;
 }
-// The result [..., n] like x, new or the caller's; its row stride.
-at::Tensor result_like(PyObject* out, const at::Tensor& x, int64_t n, at::ScalarType type, int64_t* stride) {
+// Whether rows of nx bytes from x and of ny bytes from y, `count` of each, share a byte.  Of rows that are apart
+// by different strides only the outer bounds are compared.
+bool overlap(uintptr_t x, int64_t nx, int64_t dx, uintptr_t y, int64_t ny, int64_t dy, int64_t count) {
+  if (count < 1 || x + (count - 1) * dx + nx <= y || y + (count - 1) * dy + ny <= x) return false;
+  if (count == 1 || dx != dy) return true;
+  const int64_t apart = (((int64_t)(y - x)) % dx + dx) % dx;      // columns of the same rows
+  return apart < nx || apart + ny > dx;
+}
+// The result [..., n] like x, new or the caller's; its row stride.  Blocks read all of x while others write.
+at::Tensor result_like(PyObject* out, const at::Tensor& x, const Rows& from, int64_t n, at::ScalarType type,
+                       int64_t* stride) {
   c10::DimVector shape(x.sizes().begin(), x.sizes().end());
   shape.back() = n;
   *stride = n;
@@ -201,6 +211,11 @@ at::Tensor result_like(PyObject* out, const at::Tensor& x, int64_t n, at::Scalar
   const bool rows = y.dim() == 2 && (y.size(1) <= 1 || y.stride(1) == 1) && (y.size(0) <= 1 || y.stride(0) >= n);
   if (!rows && !y.is_contiguous()) refuse(PyExc_ValueError, "out must be contiguous, or rows of contiguous elements");
   if (rows && y.size(0) > 1) *stride = y.stride(0);
+  const int64_t bx = x.element_size(), by = y.element_size();
+  if (overlap(reinterpret_cast<uintptr_t>(from.data), x.size(-1) * bx, from.stride * bx,
+              reinterpret_cast<uintptr_t>(y.const_data_ptr()), n * by, *stride * by, from.count))
+    refuse(PyExc_ValueError, "out may not overlap x");
+  y.unsafeGetTensorImpl()->bump_version();      // autograd sees that y was written
   return y;
 }
 void want(const char* name, Py_ssize_t got, Py_ssize_t n) {
@@ -290,7 +305,7 @@ PyObject* linear_w4(PyObject*, PyObject* const* a, Py_ssize_t n) {
     if ((d.y_dtype == WINO_INT8) != (a[4] != Py_None))
       refuse(PyExc_ValueError, "q_Y belongs to int8 results, and to those only");
     const float* bias = float_vector(a[2], d.w.K, x.device(), "bias must be contiguous float32 [K] on the device of x");
-    at::Tensor y = result_like(a[6], x, d.w.K, type, &d.y_stride);
+    at::Tensor y = result_like(a[6], x, r, d.w.K, type, &d.y_stride);
     void* to = y.mutable_data_ptr();
     const cudaStream_t st = c10::cuda::getCurrentCUDAStream(x.device().index()).stream();
     int rc;
@@ -338,7 +353,7 @@ PyObject* experts_w4(PyObject*, PyObject* const* a, Py_ssize_t n) {
     const Rows r = rows_of(x, d.D, keep);
     d.T = (int32_t)r.count; d.x_stride = r.stride;
     const float* bias = float_vector(a[6], d.E, x.device(), "router_bias must be contiguous float32 [E] on the device of x");
-    at::Tensor y = result_like(a[8], x, d.D, x.scalar_type(), &d.y_stride);
+    at::Tensor y = result_like(a[8], x, r, d.D, x.scalar_type(), &d.y_stride);
     c10::DimVector shape(x.sizes().begin(), x.sizes().end());
     shape.back() = top_k;
     at::Tensor ids = at::detail::empty_cuda(shape, at::kInt, x.device(), std::nullopt);

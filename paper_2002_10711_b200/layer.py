@@ -187,7 +187,8 @@ def quantize_w4(weight: torch.Tensor, group: int = 128, symmetric: bool = True, 
     """4-bit codes of `weight` ([K, C] or [E, K, C]; float32, bfloat16 or float16, on the GPU), with a scale,
     and unless `symmetric` a zero, for every `group` consecutive inputs (32, 64 or a multiple of 128).  The
     rules are wino_quantize_weights'.  Returns a W4; with values=True also the values that the codes stand
-    for, in the weights' type (what quantization-aware training puts in the weights' place)."""
+    for, in the weights' type (what quantization-aware training puts in the weights' place).  No gradient goes
+    through it: with `v` the values, `weight + (v - weight).detach()` passes one straight through."""
     codes, scales, zeros, K, C, back = _w4_result(
         _native_torch.quantize_w4(weight, group, symmetric, scale_dtype, values), "wino_quantize_weights")
     w = W4(codes, scales, zeros, K, C, group)
@@ -200,8 +201,9 @@ def linear_w4(x: torch.Tensor, w, bias: Optional[torch.Tensor] = None, q_x=None,
 
     x is float32, bfloat16 or float16, or int8 codes with their quantizer q_x (scale, zero_point), as a
     convolution of this package leaves them.  The result has x's type (float32 for codes), `out_dtype`, or
-    with q_Y int8 codes.  out: a tensor to write to, whose rows may be strided.  Made for few rows; forward
-    only (inputs that ask for a gradient are refused).  Runs on the current stream of x's device."""
+    with q_Y int8 codes.  out: a tensor to write to, whose rows may be strided, and which may not overlap x.
+    Made for few rows; forward only (inputs and scales that ask for a gradient are refused).  Runs on the current
+    stream of x's device."""
     return _w4_result(_native_torch.linear_w4(x, w, bias, q_x, q_Y, out_dtype, out), "wino_linear_forward")
 
 
@@ -213,8 +215,8 @@ def experts_w4(x: torch.Tensor, router: torch.Tensor, gate, up, down, top_k: int
 
     router [E, D] has x's type (float32, bfloat16 or float16); gate and up are W4 batches [E, I, D], down
     [E, D, I].  normalize: weights of a token add up to one.  router_bias float32 [E]: -inf takes an expert
-    out.  Returns (y [..., D] of x's type, ids int32 [..., top_k], weights float32 [..., top_k]).  Forward
-    only.  Runs on the current stream of x's device."""
+    out.  Returns (y [..., D] of x's type, ids int32 [..., top_k], weights float32 [..., top_k]).  out may not
+    overlap x.  Forward only.  Runs on the current stream of x's device."""
     return _w4_result(_native_torch.experts_w4(x, router, gate, up, down, top_k, router_bias, normalize, out),
                       "wino_experts_forward")
 

@@ -516,6 +516,32 @@ def test_refusals_on_the_gpu():
             bad()
 
 
+def test_out_beside_x():
+    """out and x as columns of one tensor; a shared byte is refused; autograd learns that out was written."""
+    rng = np.random.default_rng(31)
+    w, _ = _weights(rng, 24, 40, 32)
+    both = torch.zeros(3, 72, dtype=BF, device="cuda")
+    x, y, gap = both[:, 8:48], both[:, 48:72], both[:, :8].clone()
+    x.copy_(_inputs(rng, (3, 40), BF))
+    want, version = layer.linear_w4(x.clone(), w), both._version
+    assert layer.linear_w4(x, w, out=y) is y and both._version == version + 1
+    assert torch.equal(y, want) and torch.equal(both[:, :8], gap)
+    flat = torch.zeros(400, dtype=BF, device="cuda")
+    for bad in (lambda: layer.linear_w4(x, w, out=both[:, 47:71]), lambda: layer.linear_w4(x, w, out=both[:, :24]),
+                lambda: layer.linear_w4(x, w, out=x[:, :24]),
+                lambda: layer.linear_w4(flat[:120].view(3, 40), w, out=flat[119:191].view(3, 24)),
+                lambda: layer.linear_w4(flat[71:191].view(3, 40), w, out=flat[:72].view(3, 24)),
+                lambda: layer.linear_w4(x, w._replace(scales=w.scales.clone().requires_grad_()))):
+        with pytest.raises(ValueError):
+            bad()
+    layer.linear_w4(flat[:120].view(3, 40), w, out=flat[120:192].view(3, 24))
+    layer.linear_w4(flat[72:192].view(3, 40), w, out=flat[:72].view(3, 24))
+    gate, up, down = _small_layer(rng)
+    xe, r = _inputs(rng, (2, 64), BF).cuda(), torch.zeros(6, 64, dtype=BF, device="cuda")
+    with pytest.raises(ValueError):
+        layer.experts_w4(xe, r, gate, up, down, 2, out=xe)
+
+
 def test_a_network_with_its_head():
     """The library's convolution, pooled int8 codes, the 4-bit classifier, and an experts layer on real values."""
     gen = torch.Generator().manual_seed(21)
