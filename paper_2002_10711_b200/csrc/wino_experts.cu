@@ -2,7 +2,7 @@
 //
 // Bound by reading the chosen experts' codes, each once.  Three launches, each starting while the one in
 // front of it ends:
-//   route  a block per token: its logits, the top_k experts and their weights
+//   route  a cluster per token: its logits, the top_k experts and their weights
 //   up     a block per chosen expert and up to 8 row tiles of 16 of its inner values: gate and up products of up
 //          to 8 NT of the expert's tokens at a time, h = weight * silu(gate) * up, kept as the sum of two bf16 (three for 32-bit
 //          inputs), which the next product takes as it is: 16 (24) significant bits, so that nothing
@@ -10,6 +10,8 @@
 //   down   a block (or cluster) per up to 8 row tiles of outputs: the products of every chosen expert, summed
 //          over experts in their order; the warps of a row tile share the tiles of all experts
 // Warps stream their tiles through rings of asynchronous copies, as in the linear layer.
+// 16 tokens, 8 of 64 experts, 2048 x 1024, bf16: 78 us for the three, where the bytes alone take 28 at the rate of a
+// copy; up and down are bound by unpacking (170 and 240 instructions a 1 KB tile).  One token: 18.7 us, latency.
 // A token chooses an expert at most once, so that an expert's tokens are a set of bits, which every block
 // makes for itself from the ids: no counters, no atomics on global memory, sums in a fixed order.
 #include <cooperative_groups.h>
@@ -284,7 +286,7 @@ k_experts_up(const __grid_constant__ ExpertsArgs a, int log_split) {
                               stream_of(expert_of(a.up, expert, a.gate_units, a.gate_scales), tile_K)};
       tiles.start(from, a.gate, c0, c1, lane);
     }
-#pragma unroll 1                  // (code that runs once is waited for, about ten cycles an instruction)
+#pragma unroll 1
     for (int d = 0; d < kUpDepth; ++d) {
       if (slot < lists.chosen && c0 + d < c1) tiles.fill(ring + d * Tiles::kSlot, lane);
       Tiles::commit();

@@ -5,6 +5,9 @@
 // rows of x, which it reads from the L1 cache in the form of MMA operands.  `split` warps of a block, and the
 // S blocks of a cluster where there are too few outputs to fill the GPU, share the inputs; their sums
 // meet in shared memory in a fixed order: no workspace, no atomics.
+// One row of 8192 x 32768 in bf16: 34.9 us, where the bytes alone take 21.2 at the rate of a copy.  What is between
+// is unpacking: 155 instructions a 1 KB tile, 2.3 issued a clock, the ALU pipe busy half of the time.  The
+// row tiles of a warp share the loads of x.
 #include <cooperative_groups.h>
 
 #include "wino_packed.cuh"
