@@ -116,7 +116,6 @@ template <bool VEC, int DT, int NT, bool SMALL, bool ZEROS>
 int launch_rows(const LinearArgs& given, int num_sms, cudaStream_t st) {
   LinearArgs a = given;
   const long units = ((a.w.K + 15) / 16 + kRowTiles - 1) / kRowTiles, slices = (a.M + NT * 8 - 1) / (NT * 8);
-  if (slices > 65535) return WINO_ERR_UNSUPPORTED;
   // Inputs shared by as many warps as two blocks an SM have: split of a block times S of a cluster.
   const long room = 2l * kRowsWarps * num_sms;
   int S = 1, best = 0;

@@ -352,7 +352,6 @@ k_linear_tc(const __grid_constant__ LinearArgs a, const __grid_constant__ CUtens
 template <bool F16, int NP, bool SMALL, bool ZEROS>
 int launch_tc(const LinearArgs& a, int num_sms, int device, int* status, cudaStream_t st) {
   const long blocks = (a.w.K + 127) / 128, slices = (a.M + NP - 1) / NP;
-  if (slices > 65535) return WINO_ERR_UNSUPPORTED;
   // blocks that share the inputs, while there are SMs for them and two chunks for each; of clusters of more than
   // four, one to an SM, the GPU holds no more than fourteen at once (2048 x 2048: 10 us in sixteen of eight)
   const int most = blocks * slices <= 14 ? 8 : 4;

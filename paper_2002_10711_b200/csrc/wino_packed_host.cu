@@ -83,7 +83,15 @@ int wino_linear_forward(const wino_linear_desc_t* d, const void* x, const float*
     return WINO_ERR_ALIGNMENT;
   int sms = 0;
   if ((rc = device_sms(&sms)) != WINO_OK) return rc;
-  return launch_linear(*d, x, bias, y, sms, (cudaStream_t)stream);
+  // A grid's second dimension holds 65535 slices of 8 rows or more: more rows go in several launches.
+  constexpr int32_t kMost = 1 << 18;
+  wino_linear_desc_t part = *d;
+  for (int32_t m = 0; m < d->M && rc == WINO_OK; m += kMost) {
+    part.M = d->M - m < kMost ? d->M - m : kMost;
+    rc = launch_linear(part, static_cast<const char*>(x) + m * d->x_stride * bytes_of(d->x_dtype), bias,
+                       static_cast<char*>(y) + m * d->y_stride * bytes_of(d->y_dtype), sms, (cudaStream_t)stream);
+  }
+  return rc;
 }
 
 static int check_experts(const wino_experts_desc_t* d) {

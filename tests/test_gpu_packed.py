@@ -516,6 +516,21 @@ def test_refusals_on_the_gpu():
             bad()
 
 
+@pytest.mark.parametrize("dtype,C,K", [(F32, 33, 3), (BF, 40, 17)])
+def test_more_rows_than_a_grid_has_slices(dtype, C, K):
+    """Each row's result depends on that row alone: the same bits as in a small call with the same rows."""
+    rng = np.random.default_rng(C)
+    w, _ = _weights(rng, K, C, 32)
+    M = 524288 + 5
+    few = _inputs(rng, (41, C), dtype).cuda()
+    x = few[torch.arange(M, device="cuda") % 41]
+    out = torch.full((M, K + 2), 7.0, dtype=dtype, device="cuda")
+    layer.linear_w4(x, w, out=out[:, :K])
+    want = layer.linear_w4(few.repeat(128, 1), w)          # rows enough for the same kernel
+    assert torch.equal(out[:, :K], want[torch.arange(M, device="cuda") % 41])
+    assert (out[:, K:] == 7).all()
+
+
 def test_out_beside_x():
     """out and x as columns of one tensor; a shared byte is refused; autograd learns that out was written."""
     rng = np.random.default_rng(31)
