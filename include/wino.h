@@ -291,7 +291,9 @@ int wino_direct_last_status(void* stream);
  *
  * Arithmetic.  A weight is (code - zero) * scale, code 0..15.  Products of codes less zeros with the
  * inputs are exact and summed in 32-bit floats, a group's sum is multiplied by its scale, groups are
- * summed in 32-bit floats, and the result is rounded once, to the output's type.
+ * summed in 32-bit floats, and the result is rounded once, to the output's type.  The mixture of experts rounds once
+ * more: between its two products the inner values a_e silu(gate) * up are, for bf16 and fp16 inputs of more
+ * than two tokens, the sum of two bf16 (each rounded to nearest: off by at most 2^-17 of the value), else 32-bit floats.
  *
  * Packed form (wino_packed_t), K outputs, C inputs, tiles of 16 outputs x 128 inputs:
  *   codes   uint8 [K/16][C/128][16][4][16] (K, C rounded up): the 16 bytes at [a][b][r][t] hold row

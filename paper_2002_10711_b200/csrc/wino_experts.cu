@@ -4,9 +4,10 @@
 // front of it ends:
 //   route  a cluster per token: its logits, the top_k experts and their weights
 //   up     a block per chosen expert and up to 8 row tiles of 16 of its inner values: gate and up products of up
-//          to 8 NT of the expert's tokens at a time, h = weight * silu(gate) * up, kept as the sum of two bf16 (three for 32-bit
-//          inputs), which the next product takes as it is: 16 (24) significant bits, so that nothing
-//          is rounded to the output's type in between
+//          to 8 NT of the expert's tokens at a time, h = weight * silu(gate) * up, kept as the exact sum of three bf16
+//          for 32-bit inputs and for one or two tokens, whose planes take the MMA columns that would stay empty;
+//          else of two rounded to nearest, which leave out at most 2^-17 of h, 2.5e-6 of y (rms, replayed with
+//          2048 x 1024, 8 experts), where one bf16 would add a rounding of the output's own size
 //   down   a block (or cluster) per up to 8 row tiles of outputs: the products of every chosen expert, summed
 //          over experts in their order; the warps of a row tile share the tiles of all experts
 // Warps stream their tiles through rings of asynchronous copies, as in the linear layer.
@@ -38,9 +39,9 @@ struct ExpertsArgs {
   long y_row;                        // elements
   int* ids;
   float* weights;
-  uint16_t* h;                       // [parts][rows][h_row]
+  uint16_t* h;                       // [parts][rows][h_row], bf16
   long h_plane, h_row;               // elements
-  int T, D, I, E, top_k, normalize, vec, vec_router;
+  int T, D, I, E, top_k, normalize, vec, vec_router, parts;
 };
 
 __device__ __forceinline__ Packed expert_of(Packed w, int e, long units, long scales) {
@@ -256,6 +257,25 @@ __device__ __forceinline__ void build_lists(Lists& l, const ExpertsArgs& a) {
 // ---- gate and up --------------------------------------------------------------------------
 constexpr int kUpDepth = 3, kDownDepth = 3, kDownCluster = 4;
 
+// h as the sum of two or three bf16.  Two are rounded to nearest, each: the rest of the first is at most half of its
+// last place, 2^(e-8) of an h in [2^e, 2^(e+1)), and what the second leaves at most 2^(e-17), on either side.  (Cut off
+// as the three are they would leave up to 2^(e-15), always towards zero.)  Three cut off leave nothing.
+__device__ __forceinline__ void store_parts(uint16_t* to, long plane, int parts, float h) {
+  if (parts == 2) {
+    // beyond the largest bf16 the nearest is infinity: cut off there (infinities and NaN stay what they are)
+    const uint16_t first = fabsf(h) <= 0x1.FEp127f ? __bfloat16_as_ushort(__float2bfloat16_rn(h)) : (uint16_t)(__float_as_uint(h) >> 16);
+    const float rest = fabsf(h) <= 3.4028235e38f ? __fsub_rn(h, __uint_as_float((uint32_t)first << 16)) : 0.0f;
+    to[0] = first;
+    to[plane] = __bfloat16_as_ushort(__float2bfloat16_rn(rest));
+    return;
+  }
+#pragma unroll
+  for (int p = 0; p < 3; ++p) {
+    to[p * plane] = (uint16_t)(__float_as_uint(h) >> 16);
+    h = rest_of_any(h);
+  }
+}
+
 // An item is an expert, 8 / split row tiles, and 8 NT of the expert's tokens; a block takes every
 // gridDim.x-th, and has the next one's first tiles on the way while it finishes one.
 template <bool VEC, int DT, int NT, bool SMALL, bool ZEROS>
@@ -263,7 +283,6 @@ __global__ void __launch_bounds__(kExpertWarps * 32)
 k_experts_up(const __grid_constant__ ExpertsArgs a, int log_split) {
   using In = Input<DT>;
   using Tiles = Ring<2, 1, SMALL, ZEROS>;
-  constexpr int P = In::kParts == 3 ? 3 : 2;
   __shared__ Lists lists;
   extern __shared__ __align__(128) uint8_t smem[];
   float* sums = reinterpret_cast<float*>(smem + kExpertWarps * kUpDepth * Tiles::kSlot);   // [warp][token][33]
@@ -350,13 +369,8 @@ k_experts_up(const __grid_constant__ ExpertsArgs a, int log_split) {
       }
       const float silu = __fdiv_rn(gs, __fadd_rn(1.0f, expf(-gs)));
       const int row_h = first + this_n0 + m;
-      float h = i < a.I ? keep_nan(__fmul_rn(__fmul_rn(silu, us), lists.weight[row_h])) : 0.0f;
-      uint16_t* to = a.h + row_h * a.h_row + i;
-#pragma unroll
-      for (int p = 0; p < P; ++p) {
-        to[p * a.h_plane] = (uint16_t)(__float_as_uint(h) >> 16);
-        h = rest_of_any(h);
-      }
+      const float h = i < a.I ? keep_nan(__fmul_rn(__fmul_rn(silu, us), lists.weight[row_h])) : 0.0f;
+      store_parts(a.h + row_h * a.h_row + i, a.h_plane, a.parts, h);
     }
   }
 }
@@ -571,7 +585,6 @@ int launch_down_groups(const ExpertsArgs& a, long slots, int num_sms, int dev, c
 
 template <int DT, int NT>
 int launch_slice(const ExpertsArgs& a, int num_sms, cudaStream_t st) {
-  constexpr int P = Input<DT>::kParts == 3 ? 3 : 2;
   int dev = 0;
   if (cudaGetDevice(&dev) != cudaSuccess) return WINO_ERR_CUDA;
   // blocks that share a token's experts, until a warp has one, while there are SMs for them
@@ -588,8 +601,10 @@ int launch_slice(const ExpertsArgs& a, int num_sms, cudaStream_t st) {
   if ((rc = up(a, slots, num_sms, dev, st)) != 0) return rc;
   // columns for as many tokens as an expert may have of very few, else for more than it has as a rule: a
   // warp whose experts have more multiplies again, and the others wait for it
-  if (NT == 1 && a.T <= (P == 2 ? 4 : 2)) return launch_down_groups<P, 1>(a, slots, num_sms, dev, st);
-  return launch_down_groups<P, NT == 1 ? 2 : 4>(a, slots, num_sms, dev, st);
+  if (NT == 1 && a.T <= 2) return launch_down_groups<3, 1>(a, slots, num_sms, dev, st);
+  if constexpr (Input<DT>::kParts == 3) return launch_down_groups<3, NT == 1 ? 2 : 4>(a, slots, num_sms, dev, st);
+  else if (NT == 1 && a.T <= 4) return launch_down_groups<2, 1>(a, slots, num_sms, dev, st);
+  else return launch_down_groups<2, NT == 1 ? 2 : 4>(a, slots, num_sms, dev, st);
 }
 
 template <int DT>
@@ -599,12 +614,14 @@ int launch_type(const ExpertsArgs& a, int num_sms, cudaStream_t st) {
 }
 
 long h_row_of(int I) { return (I + 7l) / 8 * 8; }
-int parts_of(int dtype) { return dtype == WINO_FLOAT ? 3 : 2; }
+// of h, of a slice of T tokens (one or two: the NT == 1 of launch_type, and its first branch in launch_slice)
+int parts_of(int dtype, int T) { return dtype == WINO_FLOAT || T <= 2 ? 3 : 2; }
 
 }  // namespace
 
 size_t experts_workspace(int T, int I, int top_k, int dtype) {
-  return (size_t)(T < kSliceTokens ? T : kSliceTokens) * top_k * h_row_of(I) * 2 * parts_of(dtype);
+  const int slice = T < kSliceTokens ? T : kSliceTokens;   // a last, smaller one needs less
+  return (size_t)slice * top_k * h_row_of(I) * 2 * parts_of(dtype, slice);
 }
 
 int launch_experts(const wino_experts_desc_t& d, const void* x, const void* router, const float* router_bias, void* y,
@@ -625,6 +642,7 @@ int launch_experts(const wino_experts_desc_t& d, const void* x, const void* rout
   for (int t0 = 0; t0 < d.T; t0 += kSliceTokens) {
     a.T = d.T - t0 < kSliceTokens ? d.T - t0 : kSliceTokens;
     a.h_plane = (long)a.T * d.top_k * a.h_row;
+    a.parts = parts_of(d.dtype, a.T);
     a.x = (const char*)x + t0 * a.x_row;
     a.out.y = (char*)y + (long)t0 * a.y_row * size;
     a.ids = ids + (long)t0 * d.top_k; a.weights = weights + (long)t0 * d.top_k;

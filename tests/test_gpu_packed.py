@@ -354,6 +354,36 @@ def test_experts_without_normalization_or_bias():
     _experts_case(6, 128, 64, 10, 3, HF, normalize=False, bias=False, scale_dtype=HF)
 
 
+@pytest.mark.parametrize("dtype", [BF, HF])
+@pytest.mark.parametrize("at_once", [1, 2, 64])
+def test_experts_inner_values(at_once, dtype):
+    """5 h_a - 3 h_b of two inner values with one gate and up products 3 x and 5 x: nothing is left of them but what
+    the way between the two products loses of each, at most 2^-17 (two bf16 rounded to nearest), for one or two
+    tokens nothing."""
+    T, D, I = 64, 32, 16
+    code = lambda rows, **at: torch.tensor([[at.get(f"r{r}", {}).get(c, 8) for c in range(32)] for r in range(rows)])  # noqa: E731
+    gate = code(I, r0={1: 9}, r1={1: 9})
+    up = code(I, r0={0: 11}, r1={0: 13})
+    down = torch.full((D, I), 8)
+    down[:, 0], down[:, 1] = 13, 5
+    pack = lambda q: _on_gpu(layer.pack_w4(q[None], torch.ones(1, q.shape[0], 1).to(BF), None, 32))  # noqa: E731
+    rng = np.random.default_rng(41)
+    x = torch.zeros(T, D, dtype=dtype)
+    x[:, 0], x[:, 1] = _inputs(rng, (T,), dtype), _inputs(rng, (T,), dtype)
+    router = torch.zeros(1, D, dtype=dtype, device="cuda")
+    weights = pack(gate), pack(up), pack(down)
+    parts = [layer.experts_w4(p, router, *weights, 1) for p in x.cuda().split(at_once)]
+    y, w = torch.cat([p[0] for p in parts]), torch.cat([p[2] for p in parts])
+    assert (w == 1).all()
+    v, g = x[:, 0].double(), x[:, 1].double()
+    h = (g * torch.sigmoid(g) * v).abs()
+    # 5 |h_a| + 3 |h_b| = 30 |h|; the products silu * up are rounded to 2^-24 each, silu itself is common to both
+    lost = 0.0 if at_once <= 2 else 2.0 ** -17
+    bound = 30 * h * (lost + 2.0 ** -23) * (1 + 2.0 ** -20) * (1 + ref.half_step(dtype)) + torch.finfo(dtype).tiny * ref.half_step(dtype)
+    assert (y.double().cpu().abs() <= bound[:, None]).all()
+    assert (y != 0).any()
+
+
 def _small_layer(rng, E=6, D=64, I=32, dtype=BF):
     gate, _ = _weights(rng, I, D, 32, batch=(E,))
     up, _ = _weights(rng, I, D, 32, batch=(E,))
