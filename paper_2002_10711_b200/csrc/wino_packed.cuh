@@ -28,11 +28,12 @@ struct Packed {
   const uint8_t* zeros;   // null: 8
   int K, C, group, tiles_C, groups, scale_f16;
 };
+inline int groups_of(int C, int group) { return C / group + (C % group != 0); }   // no sum that passes 32 bits
 inline Packed packed_view(const wino_packed_t& w) {
   Packed p;
   p.codes = (const uint4*)w.codes_dev; p.scales = (const uint16_t*)w.scales_dev; p.zeros = w.zeros_dev;
   p.K = w.K; p.C = w.C; p.group = w.group; p.tiles_C = (w.C + 127) / 128;
-  p.groups = (w.C + w.group - 1) / w.group; p.scale_f16 = w.scale_dtype == WINO_FP16;
+  p.groups = groups_of(w.C, w.group); p.scale_f16 = w.scale_dtype == WINO_FP16;
   return p;
 }
 

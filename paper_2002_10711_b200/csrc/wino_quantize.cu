@@ -232,7 +232,7 @@ int launch_quantize(const wino_packed_t& o, const void* w, int w_dtype, int64_t 
   const int size = w_dtype == WINO_FLOAT ? 4 : 2;
   a.w = (const char*)w; a.w_row = (long)w_stride * size; a.values = (char*)values;
   a.K = o.K; a.C = o.C; a.group = o.group; a.tiles_C = (o.C + 127) / 128;
-  a.groups = (o.C + o.group - 1) / o.group; a.scale_f16 = o.scale_dtype == WINO_FP16;
+  a.groups = groups_of(o.C, o.group); a.scale_f16 = o.scale_dtype == WINO_FP16;
   a.vec = reinterpret_cast<uintptr_t>(w) % 16 == 0 && a.w_row % 16 == 0;
   a.vec_values = reinterpret_cast<uintptr_t>(values) % 16 == 0 && ((long)o.C * size) % 16 == 0;
   const long halves = 2l * ((o.K + 15) / 16);

@@ -506,6 +506,30 @@ def test_a_kernel_right_behind_the_one_that_makes_its_inputs():
         assert torch.equal(chain(False), want)
 
 
+@pytest.mark.parametrize("group", [1 << 24, (1 << 31) - 128])
+def test_a_group_far_longer_than_a_row(group):
+    """One scale an output, whatever the group's length: C + group passes 32 bits."""
+    rng = np.random.default_rng(17)
+    E, D, I, near = 3, 300, 260, 384
+    for symmetric in (True, False):
+        m = _inputs(rng, (40, D), BF).cuda()
+        a, va = layer.quantize_w4(m, near, symmetric, values=True)
+        b, vb = layer.quantize_w4(m, group, symmetric, values=True)
+        assert b.group == group and all(torch.equal(u, v) for u, v in zip(a[:3], b[:3]) if u is not None) and torch.equal(va, vb)
+        for M in (1, 20, 70):
+            x = _inputs(rng, (M, D), BF).cuda()
+            assert torch.equal(layer.linear_w4(x, a), layer.linear_w4(x, b))
+    wide, _ = _weights(rng, 5000, D, near, zeros=True)
+    x = _inputs(rng, (70, D), BF).cuda()                    # the tcgen05 kernel
+    assert torch.equal(layer.linear_w4(x, wide), layer.linear_w4(x, wide._replace(group=group)))
+    ws = [_weights(rng, *s, near, batch=(E,))[0] for s in ((I, D), (I, D), (D, I))]
+    router = _inputs(rng, (E, D), BF).cuda()
+    for T in (1, 9):
+        x = _inputs(rng, (T, D), BF).cuda()
+        for u, v in zip(layer.experts_w4(x, router, *ws, 2), layer.experts_w4(x, router, *(w._replace(group=group) for w in ws), 2)):
+            assert torch.equal(u, v)
+
+
 def test_refusals_on_the_gpu():
     rng = np.random.default_rng(14)
     w, _ = _weights(rng, 24, 40, 32)
