@@ -7,6 +7,7 @@
 
 #include <ATen/core/Tensor.h>
 #include <ATen/cuda/EmptyTensor.h>
+#include <c10/core/AutogradState.h>
 #include <c10/core/GradMode.h>
 #include <c10/cuda/CUDAGuard.h>
 #include <c10/cuda/CUDAStream.h>
@@ -127,6 +128,8 @@ wino_quant_t quantizer(PyObject* q) {
 void forward_only(const at::Tensor& t) {
   if (t.requires_grad() && c10::GradMode::is_enabled())
     refuse(PyExc_ValueError, "forward only: no gradient is computed (call under torch.no_grad())");
+  if (t._fw_grad(/*level=*/0).defined() && c10::AutogradState::get_tls_state().get_fw_grad_mode())
+    refuse(PyExc_ValueError, "forward only: no tangent is computed (call on the primals of dual tensors)");
 }
 
 // A tuple (codes, scales, zeros or None, K, C, group) of `batch` matrices on `device`.

@@ -202,8 +202,8 @@ def linear_w4(x: torch.Tensor, w, bias: Optional[torch.Tensor] = None, q_x=None,
     x is float32, bfloat16 or float16, or int8 codes with their quantizer q_x (scale, zero_point), as a
     convolution of this package leaves them.  The result has x's type (float32 for codes), `out_dtype`, or
     with q_Y int8 codes.  out: a tensor to write to, whose rows may be strided, and which may not overlap x.
-    Made for few rows; forward only (inputs and scales that ask for a gradient are refused).  Runs on the current
-    stream of x's device."""
+    Made for few rows; forward only (inputs and scales that ask for a gradient or carry a forward-mode tangent are
+    refused).  Runs on the current stream of x's device."""
     return _w4_result(_native_torch.linear_w4(x, w, bias, q_x, q_Y, out_dtype, out), "wino_linear_forward")
 
 

@@ -530,6 +530,26 @@ def test_a_group_far_longer_than_a_row(group):
             assert torch.equal(u, v)
 
 
+def test_dual_tensors_are_refused():
+    fwd = torch.autograd.forward_ad
+    rng = np.random.default_rng(18)
+    w, _ = _weights(rng, 24, 64, 32)
+    gate, up, down = _small_layer(rng)
+    x, r = _inputs(rng, (2, 64), BF).cuda(), torch.zeros(6, 64, dtype=BF, device="cuda")
+    bias, mask, out = torch.zeros(24, device="cuda"), torch.zeros(6, device="cuda"), torch.zeros(2, 24, dtype=BF, device="cuda")
+    want, (want_e, _, _) = layer.linear_w4(x, w, bias), layer.experts_w4(x, r, gate, up, down, 2, mask)
+    with fwd.dual_level():
+        dual = lambda v: fwd.make_dual(v, torch.ones_like(v))  # noqa: E731
+        for bad in (lambda: layer.linear_w4(dual(x), w), lambda: layer.linear_w4(x, w, dual(bias)),
+                    lambda: layer.linear_w4(x, w, out=dual(out)), lambda: layer.experts_w4(dual(x), r, gate, up, down, 2),
+                    lambda: layer.experts_w4(x, r, gate, up, down, 2, dual(mask))):
+            with pytest.raises(ValueError, match="tangent"):
+                bad()
+        assert torch.equal(layer.linear_w4(fwd.unpack_dual(dual(x)).primal, w, bias), want)
+    assert torch.equal(layer.linear_w4(x, w, bias), want)
+    assert torch.equal(layer.experts_w4(x, r, gate, up, down, 2, mask)[0], want_e)
+
+
 def test_refusals_on_the_gpu():
     rng = np.random.default_rng(14)
     w, _ = _weights(rng, 24, 40, 32)

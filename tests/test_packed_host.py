@@ -143,3 +143,17 @@ def test_tensor_functions_refuse_without_a_gpu():
         layer.quantize_w4(None)
     with pytest.raises(ValueError):
         layer.experts_w4(torch.zeros(1, 40), torch.zeros(2, 40), w, w, w, 1)
+
+
+def test_tangents_are_refused():
+    """Dual tensors of forward-mode derivatives: the result would have no tangent."""
+    w = layer.pack_w4(torch.zeros(4, 40, dtype=torch.uint8), torch.ones(4, 2).half(), None, 32)
+    with torch.autograd.forward_ad.dual_level():
+        dual = torch.autograd.forward_ad.make_dual(w.scales, torch.ones_like(w.scales))
+        with pytest.raises(ValueError, match="tangent"):
+            layer.linear_w4(torch.zeros(1, 40), w._replace(scales=dual))
+        router = torch.autograd.forward_ad.make_dual(torch.zeros(2, 40), torch.ones(2, 40))
+        with pytest.raises(ValueError, match="tangent"):
+            layer.experts_w4(torch.zeros(1, 40), router, w, w, w, 1)
+        with torch.no_grad(), pytest.raises(ValueError, match="tangent"):      # which does not end forward mode
+            layer.linear_w4(torch.zeros(1, 40), w._replace(scales=dual))
