@@ -71,9 +71,15 @@ struct Bad {};   // a Python exception is set
   PyErr_SetString(kind, what);
   throw Bad();
 }
-const at::Tensor& tensor(PyObject* o, const char* what) {
+// Any tensor; one that is read or written as it lies in memory.
+const at::Tensor& any_tensor(PyObject* o, const char* what) {
   if (!THPVariable_Check(o)) refuse(PyExc_TypeError, what);
   return THPVariable_Unpack(o);
+}
+const at::Tensor& tensor(PyObject* o, const char* what) {
+  const at::Tensor& t = any_tensor(o, what);
+  if (t.is_neg()) refuse(PyExc_ValueError, "a view whose elements are to be negated (call resolve_neg())");
+  return t;
 }
 long integer(PyObject* o, const char* what) {
   const long v = PyLong_Check(o) ? PyLong_AsLong(o) : (refuse(PyExc_TypeError, what), 0l);
@@ -184,7 +190,8 @@ Rows rows_of(const at::Tensor& x, int64_t n, at::Tensor& keep) {
   forward_only(x);
   Rows r;
   r.count = x.numel() / n;
-  if (x.dim() == 1 && x.stride(0) == 1) r.stride = n;
+  if (x.is_neg()) keep = x.resolve_neg().contiguous(), r.stride = n;
+  else if (x.dim() == 1 && x.stride(0) == 1) r.stride = n;
   else if (x.dim() == 2 && x.stride(1) == 1 && (x.size(0) <= 1 || x.stride(0) >= n)) r.stride = x.size(0) <= 1 ? n : x.stride(0);
   else if (x.is_contiguous()) r.stride = n;
   else keep = x.contiguous(), r.stride = n;
@@ -235,7 +242,7 @@ PyObject* quantize_w4(PyObject*, PyObject* const* a, Py_ssize_t n) {
   HANDLE_TH_ERRORS
   try {
     want("quantize_w4", n, 5);
-    const at::Tensor& given = tensor(a[0], "weight must be a tensor");
+    const at::Tensor given = any_tensor(a[0], "weight must be a tensor").resolve_neg();
     const long group = integer(a[1], "group must be an int of 32 bits");
     const bool symmetric = truth(a[2]), values = truth(a[4]);
     if (!THPDtype_Check(a[3])) refuse(PyExc_TypeError, "scale_dtype must be a torch dtype");
@@ -286,7 +293,7 @@ PyObject* linear_w4(PyObject*, PyObject* const* a, Py_ssize_t n) {
   HANDLE_TH_ERRORS
   try {
     want("linear_w4", n, 7);
-    const at::Tensor& x = tensor(a[0], "x must be a tensor");
+    const at::Tensor& x = any_tensor(a[0], "x must be a tensor");
     wino_linear_desc_t d;
     d.w = packed(a[1], 1, x.device());
     at::Tensor keep;
@@ -328,7 +335,7 @@ PyObject* experts_w4(PyObject*, PyObject* const* a, Py_ssize_t n) {
   HANDLE_TH_ERRORS
   try {
     want("experts_w4", n, 9);
-    const at::Tensor& x = tensor(a[0], "x must be a tensor");
+    const at::Tensor& x = any_tensor(a[0], "x must be a tensor");
     const at::Tensor& router = tensor(a[1], "router must be a tensor");
     wino_experts_desc_t d;
     if (router.dim() != 2 || router.size(0) < 1 || router.size(1) < 1 || router.size(0) > 512 || router.size(1) > (1 << 24) ||

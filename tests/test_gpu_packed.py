@@ -550,6 +550,29 @@ def test_dual_tensors_are_refused():
     assert torch.equal(layer.experts_w4(x, r, gate, up, down, 2, mask)[0], want_e)
 
 
+def test_pending_negations():
+    rng = np.random.default_rng(19)
+    w, _ = _weights(rng, 24, 64, 32)
+    gate, up, down = _small_layer(rng)
+    r = _inputs(rng, (6, 64), F32).cuda()
+    z = torch.complex(_inputs(rng, (3, 64), F32), _inputs(rng, (3, 64), F32)).cuda()
+    for x in (torch._neg_view(z.real.clone()), z.conj().imag, torch._neg_view(z.real.clone())[1]):
+        assert x.is_neg()
+        plain = x.resolve_neg().contiguous()
+        assert torch.equal(layer.linear_w4(x, w), layer.linear_w4(plain, w))
+        for u, v in zip(layer.experts_w4(x, r, gate, up, down, 2), layer.experts_w4(plain, r, gate, up, down, 2)):
+            assert torch.equal(u, v)
+    weight = torch._neg_view(_inputs(rng, (20, 64), BF).cuda())
+    for u, v in zip(layer.quantize_w4(weight, 32, False), layer.quantize_w4(weight.resolve_neg(), 32, False)):
+        assert torch.equal(u, v) if isinstance(u, torch.Tensor) else u == v
+    x, neg = plain.clone(), torch._neg_view
+    for bad in (lambda: layer.linear_w4(x, w, neg(torch.zeros(24, device="cuda"))),
+                lambda: layer.linear_w4(x, w, out=neg(torch.zeros(24, device="cuda"))),
+                lambda: layer.experts_w4(x, r, gate, up, down, 2, neg(torch.zeros(6, device="cuda")))):
+        with pytest.raises(ValueError, match="resolve_neg"):
+            bad()
+
+
 def test_refusals_on_the_gpu():
     rng = np.random.default_rng(14)
     w, _ = _weights(rng, 24, 40, 32)

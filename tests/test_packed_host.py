@@ -157,3 +157,15 @@ def test_tangents_are_refused():
             layer.experts_w4(torch.zeros(1, 40), router, w, w, w, 1)
         with torch.no_grad(), pytest.raises(ValueError, match="tangent"):      # which does not end forward mode
             layer.linear_w4(torch.zeros(1, 40), w._replace(scales=dual))
+
+
+def test_pending_negations_are_refused():
+    """Views whose elements torch negates when they are read (imaginary parts of conjugates)."""
+    q, s, z = torch.zeros(4, 40, dtype=torch.uint8), torch.ones(4, 2).half(), torch.zeros(4, 2, dtype=torch.uint8)
+    w = layer.pack_w4(q, s, z, 32)
+    x, neg = torch.zeros(1, 40), torch._neg_view
+    for bad in (w._replace(scales=neg(w.scales)), w._replace(zeros=neg(w.zeros)), w._replace(codes=neg(w.codes))):
+        with pytest.raises(ValueError, match="resolve_neg"):
+            layer.linear_w4(x, bad)
+    with pytest.raises(ValueError, match="resolve_neg"):
+        layer.experts_w4(x, neg(torch.zeros(2, 40)), w, w, w, 1)
