@@ -120,6 +120,7 @@ double number(PyObject* q, const char* name, double fallback) {
 int32_t whole(PyObject* q, const char* name, double fallback) {
   const double d = number(q, name, fallback);
   if (!(d >= -2147483648.0 && d <= 2147483647.0)) refuse(PyExc_ValueError, "quantizer field out of range");
+  if (d != (double)(int32_t)d) refuse(PyExc_ValueError, "zero point and code bounds of a quantizer must be whole numbers");
   return (int32_t)d;
 }
 wino_quant_t quantizer(PyObject* q) {

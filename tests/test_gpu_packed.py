@@ -573,6 +573,20 @@ def test_pending_negations():
             bad()
 
 
+def test_quantizer_fields_are_whole_numbers():
+    rng = np.random.default_rng(20)
+    w, _ = _weights(rng, 24, 64, 32)
+    x = _inputs(rng, (3, 64), I8).cuda()
+    for bad in (dict(q_x=dict(scale=0.1, zero_point=3.7)), dict(q_x=dict(scale=0.1, qmin=-0.5)),
+                dict(q_x=dict(scale=0.1), q_Y=dict(scale=0.1, zero_point=-0.25)),
+                dict(q_x=dict(scale=0.1), q_Y=dict(scale=0.1, qmax=99.5)), dict(q_x=dict(scale=0.1, zero_point=float("nan")))):
+        with pytest.raises(ValueError):
+            layer.linear_w4(x, w, **bad)
+    want = layer.linear_w4(x, w, q_x=dict(scale=0.1, zero_point=3))
+    for three in (3.0, np.int64(3), np.float32(3)):
+        assert torch.equal(layer.linear_w4(x, w, q_x=dict(scale=0.1, zero_point=three)), want)
+
+
 def test_refusals_on_the_gpu():
     rng = np.random.default_rng(14)
     w, _ = _weights(rng, 24, 40, 32)
