@@ -269,18 +269,24 @@ PyObject* quantize_w4(PyObject*, PyObject* const* a, Py_ssize_t n) {
     if (!symmetric) zeros = at::detail::empty_cuda(scale_shape, at::kByte, w.device(), std::nullopt);
     if (values) back = at::detail::empty_cuda(w.sizes(), w.scalar_type(), w.device(), std::nullopt);
     const cudaStream_t st = c10::cuda::getCurrentCUDAStream(w.device().index()).stream();
-    const int64_t size = w.element_size(), row = w.stride(-2), code_bytes = tK * tC * 1024, count = tK * groups * 16;
-    for (int64_t e = 0; e < E; ++e) {
+    const int64_t size = w.element_size(), row = K == 1 ? C : w.stride(-2), code_bytes = tK * tC * 1024, count = tK * groups * 16;
+    uint8_t* const to_codes = codes.data_ptr<uint8_t>();
+    uint8_t* const to_zeros = symmetric ? nullptr : zeros.data_ptr<uint8_t>();
+    char* const to_scales = static_cast<char*>(scales.data_ptr());
+    char* const to_values = values ? static_cast<char*>(back.data_ptr()) : nullptr;
+    const char* const from = static_cast<const char*>(w.const_data_ptr());
+    int rc = WINO_OK;
+    Py_BEGIN_ALLOW_THREADS   // a launch may wait for room in the queue
+    for (int64_t e = 0; e < E && rc == WINO_OK; ++e) {
       wino_packed_t p;
       p.K = (int32_t)K; p.C = (int32_t)C; p.group = (int32_t)group; p.scale_dtype = type_code(scale_type);
-      p.codes_dev = codes.data_ptr<uint8_t>() + e * code_bytes;
-      p.scales_dev = static_cast<char*>(scales.data_ptr()) + e * count * 2;
-      p.zeros_dev = symmetric ? nullptr : zeros.data_ptr<uint8_t>() + e * count;
-      void* v = values ? static_cast<char*>(back.data_ptr()) + e * K * C * size : nullptr;
-      const int rc = wino_quantize_weights(&p, static_cast<const char*>(w.const_data_ptr()) + e * K * C * size, code,
-                                           K == 1 ? C : row, v, st);
-      if (rc != WINO_OK) return PyLong_FromLong(rc);
+      p.codes_dev = to_codes + e * code_bytes;
+      p.scales_dev = to_scales + e * count * 2;
+      p.zeros_dev = symmetric ? nullptr : to_zeros + e * count;
+      rc = wino_quantize_weights(&p, from + e * K * C * size, code, row, values ? to_values + e * K * C * size : nullptr, st);
     }
+    Py_END_ALLOW_THREADS
+    if (rc != WINO_OK) return PyLong_FromLong(rc);
     return Py_BuildValue("(NNNLLN)", THPVariable_Wrap(codes), THPVariable_Wrap(scales), tensor_or_none(zeros),
                          (long long)K, (long long)C, tensor_or_none(back));
   } catch (const Bad&) {

@@ -587,6 +587,36 @@ def test_quantizer_fields_are_whole_numbers():
         assert torch.equal(layer.linear_w4(x, w, q_x=dict(scale=0.1, zero_point=three)), want)
 
 
+def test_other_threads_run_while_a_batch_is_quantized():
+    """One launch an expert, and the queue holds about a thousand: a call that waits for room lets others run."""
+    import sys
+    import threading
+    import time
+    w = torch.randn(6000, 16, 64, device="cuda").to(BF)
+    layer.quantize_w4(w[:2], 32)
+    torch.cuda.synchronize()
+    turns, over, interval = [0], threading.Event(), sys.getswitchinterval()
+
+    def other():
+        while not over.is_set():
+            turns[0] += 1
+            time.sleep(0)                  # hands the interpreter on by itself
+    thread = threading.Thread(target=other)
+    sys.setswitchinterval(30.0)            # nobody takes it from the caller
+    try:
+        thread.start()
+        before = turns[0]
+        got = layer.quantize_w4(w, 32)
+        after = turns[0]
+    finally:
+        over.set()
+        sys.setswitchinterval(interval)
+        thread.join()
+    assert after > before
+    for e in (0, 2999, 5999):
+        assert torch.equal(got.codes[e], layer.quantize_w4(w[e], 32).codes)
+
+
 def test_refusals_on_the_gpu():
     rng = np.random.default_rng(14)
     w, _ = _weights(rng, 24, 40, 32)
