@@ -335,7 +335,7 @@ int wino_quantize_weights(const wino_packed_t* out, const void* w_dev, int32_t w
  * point) is read for WINO_INT8 only.  y [M][K], rows y_stride elements apart, of y_dtype; for WINO_INT8
  * through q_Y as everywhere in this library: Q(fmaf(sum, s_x/s_Y, bias/s_Y); 1).  Rows of x and y need the
  * alignment of their elements only (16 bytes and multiples of 16 are faster).  M = 0 is no work.
- * Elements of y between rows are left as they are; y may not overlap x. */
+ * Elements of y between rows are left as they are; y may not overlap x, the weights or the bias. */
 typedef struct {
   int32_t M, x_dtype, y_dtype;
   int64_t x_stride, y_stride;
@@ -357,7 +357,7 @@ int wino_linear_forward(const wino_linear_desc_t* desc, const void* x_dev, const
  * ids int32 [T][top_k] and weights float [T][top_k] receive S, largest first, and a.
  * E <= 512, top_k <= 16.  Any T; the layer is laid out for few tokens (up to 64 go through the experts at
  * once, and an expert's weights are read once for 8 or, where it has more, 16 of its tokens).  T = 0 is no work.
- * y may not overlap x.  workspace_dev: wino_experts_workspace_bytes, 16-byte aligned, not shared by calls that
+ * What is written may not overlap an input.  workspace_dev: wino_experts_workspace_bytes, 16-byte aligned, not shared by calls that
  * may overlap. */
 typedef struct {
   int32_t T, D, I, E, top_k, normalize, dtype;

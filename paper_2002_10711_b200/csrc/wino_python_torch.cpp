@@ -5,6 +5,8 @@
 // which took 2.3 of the 5.5 us of a small layer's pass.
 #include <Python.h>
 
+#include <initializer_list>
+
 #include <ATen/core/Tensor.h>
 #include <ATen/cuda/EmptyTensor.h>
 #include <c10/core/AutogradState.h>
@@ -208,6 +210,24 @@ bool overlap(uintptr_t x, int64_t nx, int64_t dx, uintptr_t y, int64_t ny, int64
   const int64_t apart = (((int64_t)(y - x)) % dx + dx) % dx;      // columns of the same rows
   return apart < nx || apart + ny > dx;
 }
+// Whether the n bytes at p share one with the rows of ny bytes at y, `count` of them dy >= ny apart.
+bool touches(uintptr_t p, int64_t n, uintptr_t y, int64_t ny, int64_t dy, int64_t count) {
+  if (n < 1 || count < 1 || p + n <= y || y + (count - 1) * dy + ny <= p) return false;
+  const int64_t i = p < y || count == 1 ? 0 : (int64_t)(p - y) / dy;      // the last row that begins at or in front of p
+  return p < y + i * dy + ny || (i + 1 < count && y + (i + 1) * dy < p + n);
+}
+// The caller's result may not lie on the other operands either, dense and null where there is none: blocks read
+// them while others write.
+struct Dense { const void* data; int64_t bytes; };
+void apart(const at::Tensor& y, int64_t stride, int64_t count, int64_t n, std::initializer_list<Dense> operands) {
+  const int64_t size = y.element_size();
+  for (const Dense& o : operands)
+    if (o.data != nullptr && touches(reinterpret_cast<uintptr_t>(o.data), o.bytes, reinterpret_cast<uintptr_t>(y.const_data_ptr()),
+                                     n * size, stride * size, count))
+      refuse(PyExc_ValueError, "out may not overlap the weights, the router or a bias");
+}
+int64_t code_bytes(const wino_packed_t& w) { return (int64_t)wino_packed_code_bytes(w.K, w.C); }
+int64_t scale_count(const wino_packed_t& w) { return (int64_t)wino_packed_scale_count(w.K, w.C, w.group); }
 // The result [..., n] like x, new or the caller's; its row stride.  Blocks read all of x while others write.
 at::Tensor result_like(PyObject* out, const at::Tensor& x, const Rows& from, int64_t n, at::ScalarType type,
                        int64_t* stride) {
@@ -226,7 +246,6 @@ at::Tensor result_like(PyObject* out, const at::Tensor& x, const Rows& from, int
   if (overlap(reinterpret_cast<uintptr_t>(from.data), x.size(-1) * bx, from.stride * bx,
               reinterpret_cast<uintptr_t>(y.const_data_ptr()), n * by, *stride * by, from.count))
     refuse(PyExc_ValueError, "out may not overlap x");
-  y.unsafeGetTensorImpl()->bump_version();      // autograd sees that y was written
   return y;
 }
 void want(const char* name, Py_ssize_t got, Py_ssize_t n) {
@@ -269,7 +288,7 @@ PyObject* quantize_w4(PyObject*, PyObject* const* a, Py_ssize_t n) {
     if (!symmetric) zeros = at::detail::empty_cuda(scale_shape, at::kByte, w.device(), std::nullopt);
     if (values) back = at::detail::empty_cuda(w.sizes(), w.scalar_type(), w.device(), std::nullopt);
     const cudaStream_t st = c10::cuda::getCurrentCUDAStream(w.device().index()).stream();
-    const int64_t size = w.element_size(), row = K == 1 ? C : w.stride(-2), code_bytes = tK * tC * 1024, count = tK * groups * 16;
+    const int64_t size = w.element_size(), row = K == 1 ? C : w.stride(-2), matrix = tK * tC * 1024, count = tK * groups * 16;
     uint8_t* const to_codes = codes.data_ptr<uint8_t>();
     uint8_t* const to_zeros = symmetric ? nullptr : zeros.data_ptr<uint8_t>();
     char* const to_scales = static_cast<char*>(scales.data_ptr());
@@ -280,7 +299,7 @@ PyObject* quantize_w4(PyObject*, PyObject* const* a, Py_ssize_t n) {
     for (int64_t e = 0; e < E && rc == WINO_OK; ++e) {
       wino_packed_t p;
       p.K = (int32_t)K; p.C = (int32_t)C; p.group = (int32_t)group; p.scale_dtype = type_code(scale_type);
-      p.codes_dev = to_codes + e * code_bytes;
+      p.codes_dev = to_codes + e * matrix;
       p.scales_dev = to_scales + e * count * 2;
       p.zeros_dev = symmetric ? nullptr : to_zeros + e * count;
       rc = wino_quantize_weights(&p, from + e * K * C * size, code, row, values ? to_values + e * K * C * size : nullptr, st);
@@ -323,6 +342,11 @@ PyObject* linear_w4(PyObject*, PyObject* const* a, Py_ssize_t n) {
       refuse(PyExc_ValueError, "q_Y belongs to int8 results, and to those only");
     const float* bias = float_vector(a[2], d.w.K, x.device(), "bias must be contiguous float32 [K] on the device of x");
     at::Tensor y = result_like(a[6], x, r, d.w.K, type, &d.y_stride);
+    const bool given = a[6] != Py_None;
+    if (given)
+      apart(y, d.y_stride, r.count, d.w.K,
+            {{d.w.codes_dev, code_bytes(d.w)}, {d.w.scales_dev, 2 * scale_count(d.w)}, {d.w.zeros_dev, scale_count(d.w)}, {bias, 4l * d.w.K}});
+    if (given) y.unsafeGetTensorImpl()->bump_version();      // autograd sees that y was written
     void* to = y.mutable_data_ptr();
     const cudaStream_t st = c10::cuda::getCurrentCUDAStream(x.device().index()).stream();
     int rc;
@@ -371,12 +395,20 @@ PyObject* experts_w4(PyObject*, PyObject* const* a, Py_ssize_t n) {
     d.T = (int32_t)r.count; d.x_stride = r.stride;
     const float* bias = float_vector(a[6], d.E, x.device(), "router_bias must be contiguous float32 [E] on the device of x");
     at::Tensor y = result_like(a[8], x, r, d.D, x.scalar_type(), &d.y_stride);
+    const bool given = a[8] != Py_None;
+    if (given) {
+      apart(y, d.y_stride, r.count, d.D, {{router.const_data_ptr(), router.numel() * router.element_size()}, {bias, 4l * d.E}});
+      for (const wino_packed_t* w : {&d.gate, &d.up, &d.down})
+        apart(y, d.y_stride, r.count, d.D, {{w->codes_dev, d.E * code_bytes(*w)}, {w->scales_dev, 2 * d.E * scale_count(*w)},
+                                            {w->zeros_dev, d.E * scale_count(*w)}});
+    }
     c10::DimVector shape(x.sizes().begin(), x.sizes().end());
     shape.back() = top_k;
     at::Tensor ids = at::detail::empty_cuda(shape, at::kInt, x.device(), std::nullopt);
     at::Tensor weights = at::detail::empty_cuda(shape, at::kFloat, x.device(), std::nullopt);
     const int64_t bytes = (int64_t)wino_experts_workspace_bytes(&d);
     const at::Tensor ws = at::detail::empty_cuda({bytes}, at::kByte, x.device(), std::nullopt);
+    if (given) y.unsafeGetTensorImpl()->bump_version();      // autograd sees that y was written
     void* to = y.mutable_data_ptr();
     int32_t* to_ids = ids.mutable_data_ptr<int32_t>();
     float* to_weights = weights.mutable_data_ptr<float>();

@@ -201,7 +201,7 @@ def linear_w4(x: torch.Tensor, w, bias: Optional[torch.Tensor] = None, q_x=None,
 
     x is float32, bfloat16 or float16, or int8 codes with their quantizer q_x (scale, zero_point), as a
     convolution of this package leaves them.  The result has x's type (float32 for codes), `out_dtype`, or
-    with q_Y int8 codes.  out: a tensor to write to, whose rows may be strided, and which may not overlap x.
+    with q_Y int8 codes.  out: a tensor to write to, whose rows may be strided, and which may not overlap an input.
     Made for few rows; forward only (inputs and scales that ask for a gradient or carry a forward-mode tangent are
     refused).  Runs on the current stream of x's device."""
     return _w4_result(_native_torch.linear_w4(x, w, bias, q_x, q_Y, out_dtype, out), "wino_linear_forward")
@@ -216,7 +216,7 @@ def experts_w4(x: torch.Tensor, router: torch.Tensor, gate, up, down, top_k: int
     router [E, D] has x's type (float32, bfloat16 or float16); gate and up are W4 batches [E, I, D], down
     [E, D, I].  normalize: weights of a token add up to one.  router_bias float32 [E]: -inf takes an expert
     out.  Returns (y [..., D] of x's type, ids int32 [..., top_k], weights float32 [..., top_k]).  out may not
-    overlap x.  Forward only.  Runs on the current stream of x's device."""
+    overlap an input.  Forward only.  Runs on the current stream of x's device."""
     return _w4_result(_native_torch.experts_w4(x, router, gate, up, down, top_k, router_bias, normalize, out),
                       "wino_experts_forward")
 

@@ -698,6 +698,55 @@ def test_out_beside_x():
         layer.experts_w4(xe, r, gate, up, down, 2, out=xe)
 
 
+def test_out_beside_the_other_operands():
+    """out between or next to weights, router and biases in one allocation is taken, a shared byte refused."""
+    rng = np.random.default_rng(32)
+    M, C, K = 3, 40, 24
+    w, _ = _weights(rng, K, C, 32, zeros=True)
+    x = _inputs(rng, (M, C), F32).cuda()
+    bias = _inputs(rng, (K,), F32).cuda()
+    want = layer.linear_w4(x, w, bias)
+    rows = torch.zeros(M, 64, device="cuda")               # out in columns 0..23, the bias right behind or in a gap
+    for at in (24, 40, 64 + 24, 2 * 64 + 24):
+        flat = torch.zeros(M * 64 + K, device="cuda")
+        b, out = flat[at:at + K], flat[:M * 64].view(M, 64)[:, :K]
+        b.copy_(bias)
+        layer.linear_w4(x, w, b, out=out)
+        assert torch.equal(out, want) and torch.equal(b, bias)
+    for at in (0, 1, 23, 41, 63, 64, 2 * 64 + 23):
+        flat = torch.zeros(M * 64 + K, device="cuda")
+        version = flat._version
+        with pytest.raises(ValueError, match="overlap"):
+            layer.linear_w4(x, w, flat[at:at + K], out=flat[:M * 64].view(M, 64)[:, :K])
+        assert flat._version == version
+    one = torch.zeros(K, device="cuda")
+    with pytest.raises(ValueError, match="overlap"):
+        layer.linear_w4(x[0], w, one, out=one)
+    for v in (w.codes, w.scales, w.zeros):
+        whole = torch.zeros(v.numel() * v.element_size() + 4 * M * K, dtype=torch.uint8, device="cuda")
+        part = whole[:v.numel() * v.element_size()].view(v.dtype).view(v.shape)
+        part.copy_(v)
+        moved = layer.W4(*(part if u is v else u for u in w))
+        behind = whole[part.numel() * part.element_size():].view(F32).view(M, K)
+        assert torch.equal(layer.linear_w4(x, moved, bias, out=behind), want) and torch.equal(part, v)
+        with pytest.raises(ValueError, match="overlap"):
+            layer.linear_w4(x, moved, bias, out=whole[-4 * M * K - 4:-4].view(F32).view(M, K))
+    E, D = 6, 64
+    gate, up, down = _small_layer(rng)
+    xe, both = _inputs(rng, (2, D), BF).cuda(), torch.zeros(E + 2, D, dtype=BF, device="cuda")
+    both[:E].copy_(_inputs(rng, (E, D), BF))
+    want, ids, weights = layer.experts_w4(xe, both[:E].clone(), gate, up, down, 2)
+    y, ids2, weights2 = layer.experts_w4(xe, both[:E], gate, up, down, 2, out=both[E:])
+    assert torch.equal(y, want) and torch.equal(ids, ids2) and torch.equal(weights, weights2)
+    mask = torch.zeros(E, device="cuda")
+    for bad in (lambda: layer.experts_w4(xe, both[:E], gate, up, down, 2, out=both[E - 1:E + 1]),
+                lambda: layer.experts_w4(xe.float(), both[:E].float(), gate, up, down, 2, rows.view(-1)[:E], out=rows.view(-1)[:2 * D].view(2, D)),
+                lambda: layer.experts_w4(xe, both[:E], gate, up, down, 2, mask, out=down.scales.view(-1)[:2 * D].view(2, D)),
+                lambda: layer.experts_w4(xe, both[:E], gate, up, down, 2, mask, out=up.codes.view(-1)[-4 * D:].view(BF).view(2, D))):
+        with pytest.raises(ValueError, match="overlap"):
+            bad()
+
+
 def test_a_network_with_its_head():
     """The library's convolution, pooled int8 codes, the 4-bit classifier, and an experts layer on real values."""
     gen = torch.Generator().manual_seed(21)
