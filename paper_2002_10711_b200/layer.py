@@ -229,7 +229,7 @@ def _by_tiles(v: torch.Tensor, fill) -> torch.Tensor:
 
 
 def pack_w4(codes: torch.Tensor, scales: torch.Tensor, zeros: Optional[torch.Tensor] = None, group: int = 128) -> W4:
-    """A W4 from codes 0..15 (any integer type) [..., K, C], scales (bfloat16 or float16) and zeros
+    """A W4 from codes 0..15 (of any type) [..., K, C], scales (bfloat16 or float16) and zeros
     [..., K, groups], as checkpoints hold them.  A rearrangement with torch, done once."""
     *batch, K, C = codes.shape
     groups = -(-C // group)
@@ -238,8 +238,8 @@ def pack_w4(codes: torch.Tensor, scales: torch.Tensor, zeros: Optional[torch.Ten
     if scales.dtype not in (torch.bfloat16, torch.float16):
         raise ValueError("scales must be bfloat16 or float16")
     for v in (codes, zeros):
-        if v is not None and v.numel() and (int(v.min()) < 0 or int(v.max()) > 15):
-            raise ValueError("codes and zeros must be 0..15")
+        if v is not None and not ((v >= 0) & (v <= 15) & (v == v.to(torch.uint8))).all():
+            raise ValueError("codes and zeros must be whole numbers 0..15")
     q = torch.nn.functional.pad(codes.to(torch.uint8), (0, -C % 128, 0, -K % 16))
     tiles_K, tiles_C, n = q.shape[-2] // 16, q.shape[-1] // 128, len(batch)
     q = q.view(*batch, tiles_K, 16, tiles_C, 4, 4, 4, 2)          # a r b i t (e / 2) (e % 2)

@@ -169,3 +169,15 @@ def test_pending_negations_are_refused():
             layer.linear_w4(x, bad)
     with pytest.raises(ValueError, match="resolve_neg"):
         layer.experts_w4(x, neg(torch.zeros(2, 40)), w, w, w, 1)
+
+
+def test_pack_takes_whole_numbers_only():
+    q, s = torch.full((4, 40), 3), torch.ones(4, 2).half()
+    want = layer.pack_w4(q, s, torch.full((4, 2), 7), 32)
+    got = layer.pack_w4(q.float(), s, torch.full((4, 2), 7.0), 32)
+    assert all(torch.equal(u, v) for u, v in zip(want[:3], got[:3]))
+    nan = torch.full((4, 2), float("nan"))
+    for bad in ((q + 0.5, s, None), (q.float().index_fill(1, torch.tensor([7]), float("nan")), s, None), (q, s, torch.full((4, 2), 6.75)),
+                (q, s, nan), (q - 4, s, None), (q + 253, s, None), (q * float("inf"), s, None)):
+        with pytest.raises(ValueError):
+            layer.pack_w4(*bad, 32)
