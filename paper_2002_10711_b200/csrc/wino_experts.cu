@@ -282,7 +282,7 @@ template <bool VEC, int DT, int NT, bool SMALL, bool ZEROS>
 __global__ void __launch_bounds__(kExpertWarps * 32)
 k_experts_up(const __grid_constant__ ExpertsArgs a, int log_split) {
   using In = Input<DT>;
-  using Tiles = Ring<2, 1, SMALL, ZEROS>;
+  using Tiles = Ring<2, SMALL, ZEROS>;
   __shared__ Lists lists;
   extern __shared__ __align__(128) uint8_t smem[];
   float* sums = reinterpret_cast<float*>(smem + kExpertWarps * kUpDepth * Tiles::kSlot);   // [warp][token][33]
@@ -303,7 +303,7 @@ k_experts_up(const __grid_constant__ ExpertsArgs a, int log_split) {
       const int tile_K = min(block_K * per_block + (warp >> log_split), tiles_K - 1), expert = lists.expert[slot];
       const Stream from[2] = {stream_of(expert_of(a.gate, expert, a.gate_units, a.gate_scales), tile_K),
                               stream_of(expert_of(a.up, expert, a.gate_units, a.gate_scales), tile_K)};
-      tiles.start(from, a.gate, c0, c1, lane);
+      tiles.start(from, a.gate, c0, lane);
     }
 #pragma unroll 1
     for (int d = 0; d < kUpDepth; ++d) {
@@ -382,7 +382,7 @@ template <int P, int NT, bool SMALL, bool ZEROS>
 __global__ void __launch_bounds__(kExpertWarps * 32)
 k_experts_down(const __grid_constant__ ExpertsArgs a, int log_split, int log_S) {
   using In = Input<WINO_BF16>;
-  using Tiles = Ring<2, 1, SMALL, ZEROS>;
+  using Tiles = Ring<2, SMALL, ZEROS>;
   constexpr int kEach = P == 2 ? 4 : 2, kTokens = NT * kEach;      // tokens of an MMA's columns, and at a time
   __shared__ Lists lists;
   extern __shared__ __align__(128) uint8_t smem[];
@@ -407,7 +407,7 @@ k_experts_down(const __grid_constant__ ExpertsArgs a, int log_split, int log_S) 
   auto start = [&](int s, int at) {
     const Packed w = expert_of(a.down, lists.expert[s], a.down_units, a.down_scales);
     const Stream of[2] = {stream_of(w, unit * 2), stream_of(w, min(unit * 2 + 1, tiles_K - 1))};
-    from.start(of, a.down, at, tiles, lane);
+    from.start(of, a.down, at, lane);
   };
   if (u0 < u1) {
     slot = fill_slot = u0 / tiles;
@@ -544,7 +544,7 @@ int log2_of(int n) {
 
 template <bool VEC, int DT, int NT, bool SMALL, bool ZEROS>
 int launch_up(const ExpertsArgs& a, long slots, int num_sms, int dev, cudaStream_t st) {
-  constexpr size_t least = (size_t)kExpertWarps * (kUpDepth * Ring<2, 1, SMALL, ZEROS>::kSlot + NT * 8 * 33 * sizeof(float));
+  constexpr size_t least = (size_t)kExpertWarps * (kUpDepth * Ring<2, SMALL, ZEROS>::kSlot + NT * 8 * 33 * sizeof(float));
   const long tiles_K = (a.I + 15) / 16;
   const int split = shared_by(tiles_K * slots, a.gate.tiles_C, kExpertWarps, kBlocksPerSm * kExpertWarps * num_sms);
   const long items = (tiles_K + kExpertWarps / split - 1) / (kExpertWarps / split) * slots;
@@ -559,7 +559,7 @@ int launch_up(const ExpertsArgs& a, long slots, int num_sms, int dev, cudaStream
 
 template <int P, int NT, bool SMALL, bool ZEROS>
 int launch_down(const ExpertsArgs& a, long slots, int num_sms, int dev, cudaStream_t st) {
-  constexpr size_t ring = (size_t)kExpertWarps * kDownDepth * Ring<2, 1, SMALL, ZEROS>::kSlot;
+  constexpr size_t ring = (size_t)kExpertWarps * kDownDepth * Ring<2, SMALL, ZEROS>::kSlot;
   const long units = ((a.D + 15) / 16 + 1) / 2;
   const int by = shared_by(units, (a.I + 127l) / 128 * slots, kDownCluster * kExpertWarps, kBlocksPerSm * kExpertWarps * num_sms);
   const int split = by < kExpertWarps ? by : kExpertWarps, S = by / split;

@@ -24,7 +24,7 @@ __global__ void __launch_bounds__(kRowsWarps * 32)
 k_linear_rows(const __grid_constant__ LinearArgs a) {
   using In = Input<DT>;
   constexpr int R = kRowTiles, kSums = R * 16 + 1;   // floats of a row of sums: one bank apart
-  using Tiles = Ring<R, 1, SMALL, ZEROS>;
+  using Tiles = Ring<R, SMALL, ZEROS>;
   extern __shared__ __align__(128) uint8_t smem[];
   const cg::cluster_group cluster = cg::this_cluster();
   const int S = (int)cluster.num_blocks(), rank = (int)cluster.block_rank();
@@ -51,7 +51,7 @@ k_linear_rows(const __grid_constant__ LinearArgs a) {
     for (int n = 0; n < NT; ++n) row[n] = a.x + min(m0 + 8 * n + g, a.M - 1) * a.x_row;
     const uint32_t ring = smem_u32(smem) + warp * kRingSlots * Tiles::kSlot, ring_end = ring + kRingSlots * Tiles::kSlot;
     Tiles tiles;
-    tiles.start(w, a.w, c0, c1, lane);
+    tiles.start(w, a.w, c0, lane);
 #pragma unroll 1
     for (int d = 0; d < kRingSlots; ++d) {
       if (c0 + d < c1) tiles.fill(ring + d * Tiles::kSlot, lane);
@@ -128,7 +128,7 @@ int launch_rows(const LinearArgs& given, int num_sms, cudaStream_t st) {
     }
   const long blocks = (units + kRowsWarps / a.split - 1) / (kRowsWarps / a.split);
   const dim3 grid((unsigned)(blocks * S), (unsigned)slices);
-  constexpr size_t ring = (size_t)kRowsWarps * kRingSlots * Ring<kRowTiles, 1, SMALL, ZEROS>::kSlot;
+  constexpr size_t ring = (size_t)kRowsWarps * kRingSlots * Ring<kRowTiles, SMALL, ZEROS>::kSlot;
   constexpr size_t sums = (size_t)2 * kRowsWarps * NT * 8 * (kRowTiles * 16 + 1) * sizeof(float);
   constexpr size_t least = ring > sums ? ring : sums;
   // no more blocks on an SM than its share: while the kernel in front runs they would gather on a few

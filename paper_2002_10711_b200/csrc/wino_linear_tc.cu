@@ -361,8 +361,7 @@ int launch_tc(const LinearArgs& a, int num_sms, int device, int* status, cudaStr
   constexpr size_t sums = (size_t)NP * 128 * sizeof(float);
   constexpr size_t smem = (ring > sums ? ring : sums) + 1024;
   CUtensorMap map_x;
-  const uint64_t row = a.M == 1 ? ((uint64_t)a.w.C * 2 + 15) / 16 * 16 : (uint64_t)a.x_row;
-  int rc = encode_rows_16bit(&map_x, a.x, F16, (uint64_t)a.w.C, (uint64_t)a.M, row, 64, NP);
+  int rc = encode_rows_16bit(&map_x, a.x, F16, (uint64_t)a.w.C, (uint64_t)a.M, (uint64_t)a.x_row, 64, NP);
   if (rc != 0) return rc;
   static DeviceOnce once;
   auto kernel = k_linear_tc<F16, NP, SMALL, ZEROS>;

@@ -269,32 +269,31 @@ __device__ __forceinline__ Stream stream_of(const Packed& w, long tile_K) {
 // A warp's ring of weight tiles in shared memory, filled by asynchronous copies several tiles ahead of
 // their use: each lane copies the two units of codes it will read itself, some lanes the scales and zeros
 // as well (SMALL, groups of 32 or 64 inputs: four or two to a tile; else a group is one or more tiles, and
-// every tile brings its scales along).  A slot holds T consecutive tiles of each of R row tiles.
-template <int R, int T, bool SMALL, bool ZEROS> struct Ring {
+// every tile brings its scales along).  A slot holds one tile of each of R row tiles.
+template <int R, bool SMALL, bool ZEROS> struct Ring {
   static constexpr int kGroups = SMALL ? 4 : 1;       // room for, a tile
-  static constexpr int kScales = R * T * 1024, kZeros = kScales + R * T * kGroups * 32;
-  static constexpr int kSlot = kZeros + (ZEROS ? R * T * kGroups * 16 : 0);
+  static constexpr int kScales = R * 1024, kZeros = kScales + R * kGroups * 32;
+  static constexpr int kSlot = kZeros + (ZEROS ? R * kGroups * 16 : 0);
   const char* codes[R];
   const char* meta[R];     // scales, or zeros, of the row tile
-  int c, end;              // next tile, and the last one's successor
+  int c;                   // next tile
   int per;                 // groups a tile (SMALL) or tiles a group
   int groups;
-  // this lane's 16 bytes of scales (two lanes a group) or zeros (a lane a group): tile of the slot, group of
-  // the tile, size of a group, offset in the group, place in the slot; tile >= T: none
-  int my_tile, my_group, my_size, my_part;
+  // this lane's 16 bytes of scales (two lanes a group) or zeros (a lane a group): whether it has some, group of
+  // the tile, size of a group, offset in the group, place in the slot
+  bool mine;
+  int my_group, my_size, my_part;
   uint32_t my_place;
 
-  // the next fill is of tiles `from` .. of `w`, none of them `to` or beyond
-  __device__ __forceinline__ void start(const Stream (&w)[R], const Packed& p, int from, int to, int lane) {
-    c = from; end = to; groups = p.groups;
+  // the next fill is of tile `from` of `w`
+  __device__ __forceinline__ void start(const Stream (&w)[R], const Packed& p, int from, int lane) {
+    c = from; groups = p.groups;
     per = SMALL ? (p.group == 32 ? 4 : 2) : p.group >> 7;
-    const int of_tile = SMALL ? per : 1;              // groups a tile
-    const bool zero = ZEROS && lane >= 2 * kGroups * T;
-    const int i = zero ? lane - 2 * kGroups * T : lane >> 1;   // group of the slot
-    my_tile = i / of_tile; my_group = i % of_tile;    // powers of two
-    if (!ZEROS && lane >= 2 * kGroups * T) my_tile = T;
+    const bool zero = ZEROS && lane >= 2 * kGroups;
+    my_group = zero ? lane - 2 * kGroups : lane >> 1;
+    mine = my_group < (SMALL ? per : 1);
     my_size = zero ? 16 : 32; my_part = zero ? 0 : 16 * (lane & 1);
-    my_place = (zero ? kZeros : kScales) + (my_tile * kGroups + my_group) * my_size + my_part;
+    my_place = (zero ? kZeros : kScales) + my_group * my_size + my_part;
 #pragma unroll
     for (int r = 0; r < R; ++r) {
       codes[r] = reinterpret_cast<const char*>(w[r].codes + c * 64l + lane);
@@ -304,27 +303,23 @@ template <int R, int T, bool SMALL, bool ZEROS> struct Ring {
   __device__ __forceinline__ void fill(uint32_t slot, int lane) {
     const uint32_t to = slot + lane * 16;
 #pragma unroll
-    for (int j = 0; j < T; ++j)
-      if (j == 0 || c + j < end)
-#pragma unroll
-        for (int r = 0; r < R; ++r) {
-          asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to + (r * T + j) * 1024), "l"(codes[r] + j * 1024) : "memory");
-          asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to + (r * T + j) * 1024 + 512), "l"(codes[r] + j * 1024 + 512) : "memory");
-        }
-    const int tile = c + my_tile;
-    const int group = SMALL ? tile * per + my_group : per == 1 ? tile : tile / per;
-    if (my_tile < T && tile < end) {
+    for (int r = 0; r < R; ++r) {
+      asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to + r * 1024), "l"(codes[r]) : "memory");
+      asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to + r * 1024 + 512), "l"(codes[r] + 512) : "memory");
+    }
+    if (mine) {
+      const int group = SMALL ? c * per + my_group : per == 1 ? c : c / per;
       // groups behind the last: zeros in place of what is not there
       const bool in = !SMALL || group < groups;
       const int bytes = in ? 16 : 0;
 #pragma unroll
       for (int r = 0; r < R; ++r)
-        asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(slot + my_place + r * T * kGroups * my_size),
+        asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(slot + my_place + r * kGroups * my_size),
                      "l"(meta[r] + (in ? group : 0) * (long)my_size), "r"(bytes) : "memory");
     }
 #pragma unroll
-    for (int r = 0; r < R; ++r) codes[r] += T * 1024;
-    c += T;
+    for (int r = 0; r < R; ++r) codes[r] += 1024;
+    ++c;
   }
   __device__ __forceinline__ static void commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
   template <int PENDING> __device__ __forceinline__ static void wait() {
@@ -353,7 +348,7 @@ __device__ __forceinline__ uint32_t word_of(const uint4& u, int i) {
   return i == 0 ? u.x : i == 1 ? u.y : i == 2 ? u.z : u.w;
 }
 
-// One 16 x 128 tile of weights, the one at `index` (r T + j) of a ring's slot, against NT x 8 rows of x: acc +=
+// One 16 x 128 tile of weights, the `index`-th of a ring's slot, against NT x 8 rows of x: acc +=
 // scale * (codes - zeros) x, the sum of a group multiplied by its scale (for groups of at least 128: of a
 // tile).  x[n][i]: the input of row 8 n + g at 32 i + 8 t.  Two chains of MMAs: one would wait for itself.
 template <bool SMALL, bool ZEROS, class Tiles, int NT, class In>
