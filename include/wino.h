@@ -334,7 +334,8 @@ int wino_quantize_weights(const wino_packed_t* out, const void* w_dev, int32_t w
 /* y = (x - z_x) s_x W^T + bias.  x [M][C], rows x_stride elements apart, of x_dtype; q_x (scale, zero
  * point) is read for WINO_INT8 only.  y [M][K], rows y_stride elements apart, of y_dtype; for WINO_INT8
  * through q_Y as everywhere in this library: Q(fmaf(sum, s_x/s_Y, bias/s_Y); 1).  Rows of x and y need the
- * alignment of their elements only (16 bytes and multiples of 16 are faster).  M = 0 is no work.
+ * alignment of their elements only, but many bf16 or fp16 rows on 16-byte boundaries are up to eight times faster.
+ * M = 0 is no work.
  * Elements of y between rows are left as they are; y may not overlap x, the weights or the bias. */
 typedef struct {
   int32_t M, x_dtype, y_dtype;
@@ -355,8 +356,9 @@ int wino_linear_forward(const wino_linear_desc_t* desc, const void* x_dev, const
  * is out gets ids 0 .. top_k-1, weights 0 and y = 0; where it has fewer than top_k experts left, the rest of its
  * ids are the lowest experts that are out, with weight 0.  A NaN or +inf among a token's logits makes its weights and y NaN.
  * ids int32 [T][top_k] and weights float [T][top_k] receive S, largest first, and a.
- * E <= 512, top_k <= 16.  Any T; the layer is laid out for few tokens (up to 64 go through the experts at
- * once, and an expert's weights are read once for 8 or, where it has more, 16 of its tokens).  T = 0 is no work.
+ * E <= 512, top_k <= 16.  Any T; the layer is laid out for few tokens: up to 64 go through the experts at once, and
+ * of each 64 an expert's down weights are read once, its gate and up weights once for every 8 of its tokens (16
+ * where T > 8 and T * top_k > 6 E).  T = 0 is no work.
  * What is written may not overlap an input.  workspace_dev: wino_experts_workspace_bytes, 16-byte aligned, not shared by calls that
  * may overlap. */
 typedef struct {

@@ -5,9 +5,13 @@
 // rows of x, which it reads from the L1 cache in the form of MMA operands.  `split` warps of a block, and the
 // S blocks of a cluster where there are too few outputs to fill the GPU, share the inputs; their sums
 // meet in shared memory in a fixed order: no workspace, no atomics.
-// One row of 8192 x 32768 in bf16: 34.9 us, where the bytes alone take 21.2 at the rate of a copy.  What is between
-// is unpacking: 155 instructions a 1 KB tile, 2.3 issued a clock, the ALU pipe busy half of the time.  The
-// row tiles of a warp share the loads of x.
+// One row of 8192 x 32768 in bf16: 34.6 us, where the bytes alone take 21.2 at the rate of a copy.  No unit is full: of
+// 155 instructions a 1 KB tile 2.3 are issued a clock while an SM has work (58 % of what it can, the ALU pipe 51 %
+// busy), and 256 blocks on 148 SMs leave 40 of them with one block where the others have two, 1.9 a clock over the whole
+// time.  Short sums are bound by latency: no weight is asked for before the kernel in front is over.  The row tiles
+// of a warp share the loads of x.
+// Rows that are not on 16-byte boundaries, or whose length is no multiple of eight, are read an element at a time and
+// eight at once: 64 rows of 8191 x 8192 in bf16 take 160 us, of 8192 x 8192 21 (on the other kernel).
 #include <cooperative_groups.h>
 
 #include "wino_packed.cuh"

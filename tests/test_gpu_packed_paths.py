@@ -127,6 +127,21 @@ def test_tcgen05_kernel_to_other_types(M):
     assert (~near).double().mean() > 0.9 and got.unique().numel() > 50
 
 
+@pytest.mark.parametrize("dtype", [BF, HF])
+@pytest.mark.parametrize("M,C,K,stride", [(64, 2043, 2600, 2048), (20, 3337, 3200, 3352), (3, 1021, 200, 1024)])
+def test_rows_with_gaps(M, C, K, stride, dtype):
+    """Rows of odd length on 16-byte boundaries: what stands between them is nobody's."""
+    rng = np.random.default_rng(C)
+    w, W = _weights(rng, K, C, 128, BF, True)
+    base = torch.full((M, stride), float("nan"), dtype=dtype)
+    base[:, :C] = _inputs(rng, (M, C), dtype)
+    x = base.cuda()[:, :C]
+    want, bound = ref.linear(base[:, :C].double(), W, None, 128)
+    _check(layer.linear_w4(x, w), want, bound, dtype)
+    assert ("k_linear_tc" if M > 8 else "k_linear_rows") in _kernels(lambda: layer.linear_w4(x, w))[0][0]
+    assert torch.equal(layer.linear_w4(x.contiguous()[:3], w), layer.linear_w4(x[:3], w))
+
+
 # --- experts -------------------------------------------------------------------------------
 @pytest.mark.parametrize("T,D,I,E,k,dtype,bias", [
     (16, 256, 1024, 64, 8, BF, 0.0),        # 512 items of the gate and up products on 296 blocks
