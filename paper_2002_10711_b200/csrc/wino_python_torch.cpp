@@ -202,19 +202,23 @@ Rows rows_of(const at::Tensor& x, int64_t n, at::Tensor& keep) {
   if (r.count > (1 << 24)) refuse(PyExc_ValueError, "more than 2^24 rows");
   return r;
 }
-// Whether rows of nx bytes from x and of ny bytes from y, `count` of each, share a byte.  Of rows that are apart
-// by different strides only the outer bounds are compared.
-bool overlap(uintptr_t x, int64_t nx, int64_t dx, uintptr_t y, int64_t ny, int64_t dy, int64_t count) {
-  if (count < 1 || x + (count - 1) * dx + nx <= y || y + (count - 1) * dy + ny <= x) return false;
-  if (count == 1 || dx != dy) return true;
-  const int64_t apart = (((int64_t)(y - x)) % dx + dx) % dx;      // columns of the same rows
-  return apart < nx || apart + ny > dx;
-}
 // Whether the n bytes at p share one with the rows of ny bytes at y, `count` of them dy >= ny apart.
 bool touches(uintptr_t p, int64_t n, uintptr_t y, int64_t ny, int64_t dy, int64_t count) {
   if (n < 1 || count < 1 || p + n <= y || y + (count - 1) * dy + ny <= p) return false;
   const int64_t i = p < y || count == 1 ? 0 : (int64_t)(p - y) / dy;      // the last row that begins at or in front of p
   return p < y + i * dy + ny || (i + 1 < count && y + (i + 1) * dy < p + n);
+}
+// The same of `count` rows of nx bytes from x, dx apart.
+bool overlap(uintptr_t x, int64_t nx, int64_t dx, uintptr_t y, int64_t ny, int64_t dy, int64_t count) {
+  if (count < 1 || x + (count - 1) * dx + nx <= y || y + (count - 1) * dy + ny <= x) return false;
+  if (count == 1) return true;
+  if (dx == dy) {
+    const int64_t apart = (((int64_t)(y - x)) % dx + dx) % dx;      // columns of the same rows
+    return apart < nx || apart + ny > dx;
+  }
+  for (int64_t i = 0; i < count; ++i)
+    if (touches(x + i * dx, nx, y, ny, dy, count)) return true;
+  return false;
 }
 // The caller's result may not lie on the other operands either, dense and null where there is none: blocks read
 // them while others write.

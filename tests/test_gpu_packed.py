@@ -747,6 +747,29 @@ def test_out_beside_the_other_operands():
             bad()
 
 
+def test_out_between_rows_of_x():
+    """Rows of x and of out at different strides in one tensor: taken where no byte is shared."""
+    rng = np.random.default_rng(33)
+    w, _ = _weights(rng, 40, 40, 32)
+    rows = torch.zeros(10, 40, dtype=BF, device="cuda")
+    for x, out in (((0, 9, 4), (1, 4, 1)), ((0, 9, 4), (5, 8, 1)), ((1, 4, 1), (0, 10, 4)), ((0, 10, 3), (1, 8, 2))):
+        xs, outs = list(range(*x))[:3], list(range(*out))[:3]
+        rows.copy_(_inputs(rng, (10, 40), BF))
+        before, v, y = rows.clone(), rows[x[0]:x[1]:x[2]][:3], rows[out[0]:out[1]:out[2]][:3]
+        if set(xs) & set(outs):
+            with pytest.raises(ValueError, match="overlap"):
+                layer.linear_w4(v, w, out=y)
+            assert torch.equal(rows, before)
+            continue
+        layer.linear_w4(v, w, out=y)
+        assert torch.equal(y, layer.linear_w4(before[xs], w))
+        rest = [r for r in range(10) if r not in outs]
+        assert torch.equal(rows[rest], before[rest])
+    flat = torch.zeros(400, dtype=BF, device="cuda")
+    with pytest.raises(ValueError, match="overlap"):       # their second rows are the same elements
+        layer.linear_w4(flat[:200].view(2, 100)[:, :40], w, out=flat[40:160].view(2, 60)[:, :40])
+
+
 def test_a_network_with_its_head():
     """The library's convolution, pooled int8 codes, the 4-bit classifier, and an experts layer on real values."""
     gen = torch.Generator().manual_seed(21)
