@@ -1,6 +1,6 @@
 // Mixture of experts for few tokens, with 4-bit weights: router, gate and up products, down product.
 //
-// Bound by reading the chosen experts' codes, each once.  Three launches, each starting while the one in
+// What it cannot do without is reading the chosen experts' codes, each once.  Three launches, each starting while the one in
 // front of it ends:
 //   route  a cluster per token: its logits, the top_k experts and their weights
 //   up     a block per chosen expert and up to 8 row tiles of 16 of its inner values: gate and up products of up

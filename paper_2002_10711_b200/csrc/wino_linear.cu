@@ -1,6 +1,6 @@
 // y = x W^T + bias with 4-bit weights and group scales, for few rows of x: warp MMAs on unpacked codes.
 //
-// Bound by reading the codes: 16 outputs x 128 inputs are 1 KB, read once.  A warp streams the tiles of R row
+// What it cannot do without is reading the codes: 16 outputs x 128 inputs are 1 KB, read once.  A warp streams the tiles of R row
 // tiles (16 R outputs) over a part of the inputs through a ring of asynchronous copies, against up to 8 NT
 // rows of x, which it reads from the L1 cache in the form of MMA operands.  `split` warps of a block, and the
 // S blocks of a cluster where there are too few outputs to fill the GPU, share the inputs; their sums

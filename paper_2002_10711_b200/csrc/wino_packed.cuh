@@ -2,8 +2,9 @@
 //
 // A code less its zero is an integer of magnitude at most 15, exact in bf16 and in fp16, and so is
 // every input of those types; int8 inputs less their zero point (at most 255 in magnitude) are exact
-// fp16 integers, and a 32-bit input is the exact sum of three bf16 values of 8 significant bits each.
-// The products are therefore exact, and the only roundings in front of the output are those of 32-bit sums.
+// fp16 integers, and a 32-bit input is the exact sum of three bf16 values of 8 significant bits each (down to 2^-110).
+// The products are therefore exact, and the only roundings in front of the output are those of 32-bit sums (and, in
+// the experts, that of the inner values between the two products).
 //
 // Warp MMA m16n8k16, weights as the 16-row operand, up to 8 rows of x as the columns.  Lane (g, t) =
 // (lane / 4, lane % 4) holds rows g and g + 8 of A and column g of B at k = 2t, 2t+1, 2t+8, 2t+9.
